@@ -263,6 +263,100 @@ int64_t onela_launch_count(const onela_ctx* ctx);
  * 0 a CUDA-core kernel (dk = dv = 32, ONELA_FLAG_FORCE_GENERIC). */
 int32_t onela_uses_tensor_core_path(const onela_ctx* ctx);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Operators around the beam decode.  They take a struct of arguments and need no context and no workspace: sizes, strides
+ * and pointers are the caller's, every call is asynchronous on `stream` (a stream of the current device), allocates nothing
+ * and can be captured in a CUDA graph.  Strides are in elements and at least the extent they step over; base pointers are
+ * 16-byte aligned and, where a stride is given, so is every row (the stride times the element size is a multiple of 16) -
+ * but for onela_sample_tokens, whose rows may start anywhere.
+ * Inputs and outputs do not overlap unless a call says so.  An empty call (no tokens, sequences or rows) does nothing. */
+
+#define ONELA_NORM_NONE 0
+#define ONELA_NORM_L2 1           /* x / sqrt(sum x^2 + eps) */
+#define ONELA_NORM_RMS 2          /* x / sqrt(mean x^2 + eps) * weight */
+
+/* Norms of queries and keys for each head and, in the same pass, the rotation by the tokens' positions: what turns a
+ * projection's output into the q and k that every other call takes as given (Gated DeltaNet layers: L2 norms, no rotation;
+ * the attention layers of a hybrid model: RMS norms with weights, the first rotary_dim elements rotated).
+ * Element pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when interleaved, i < rotary_dim / 2, turn by the angle
+ * position * inv_freq[i]: (a, b) -> (a cos - b sin, b cos + a sin).  Angles are formed in 64 bits and any int32 position is
+ * fine, negative ones included.  Queries are multiplied by q_scale at the end.  Norms and products in fp32, one rounding.
+ * q_out may be q and k_out may be k with the same stride (in place); otherwise outputs overlap nothing. */
+typedef struct onela_norm_rotate_args {
+    const void *q_dev, *k_dev;        /* [n_tokens][num_q_heads][head_dim], [n_tokens][num_k_heads][head_dim] in dtype */
+    void *q_out_dev, *k_out_dev;      /* the same shapes and dtype */
+    const float *q_weight_dev, *k_weight_dev;   /* [head_dim], ONELA_NORM_RMS only (null: ones) */
+    const int32_t* positions_dev;     /* [n_tokens]; null without rotation */
+    const float* inv_freq_dev;        /* [rotary_dim / 2]; null without rotation */
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;   /* elements between consecutive tokens */
+    int64_t n_tokens;
+    int32_t num_q_heads, num_k_heads; /* either may be 0 */
+    int32_t head_dim;                 /* a multiple of 8 up to 256 */
+    int32_t rotary_dim;               /* 0 (no rotation) or a multiple of 16 up to head_dim */
+    int32_t interleaved;
+    int32_t norm;                     /* ONELA_NORM_* */
+    int32_t dtype;                    /* ONELA_DTYPE_* */
+    float eps, q_scale;
+} onela_norm_rotate_args;
+onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream);
+
+/* The gated delta rule (Eq. 1) over ragged sequences, without beams: every sequence carries ONE state per value head from
+ * token to token and every token gets its output (which onela_prefill_shared_state does not compute),
+ *        S_t = alpha_t S_{t-1} + beta_t (v_t - alpha_t S_{t-1} k_t) k_t^T ,    o_t = S_t q_t ,
+ * prompts and single tokens (sampled generation) in the same call.  Sequence i's tokens are rows starts[i] .. starts[i + 1] - 1
+ * of q, k, v, the gates and out (starts null: row i alone); its state is states[slots[i]] (slots null: states[i]), read
+ * before its first token unless fresh[i] is set (then it starts from zero), replaced after its last, fp32.  States are [value head][dv][dk] as
+ * onela_init_shared_states takes them.  Value head j reads query and key head j / (num_v_heads / num_heads).
+ * A negative slot marks a padded sequence: nothing of it is read or written.  Rows of no sequence are left as they are.  A sequence without
+ * tokens keeps its state (or, fresh, gets the zero state).  Found on the device, with *status_dev, if given, set to {ONELA_E_DEVICE_CHECK, sequence}
+ * by one that finds it (the caller clears the words): a slot of num_states or more, or that an earlier sequence of the call has, and row
+ * ranges that run backwards, begin before an earlier sequence's or leave [0, n_tokens]; such a sequence is treated as padded.
+ * States, outputs and inputs do not overlap.
+ * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it
+ * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores.
+ * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED. */
+typedef struct onela_delta_rule_args {
+    const void *q_dev, *k_dev, *v_dev;       /* [n_tokens][num_heads][dk] twice, [n_tokens][num_v_heads][dv] in dtype */
+    const float *alpha_dev, *beta_dev;       /* [n_tokens][num_v_heads] */
+    float* states_dev;                       /* [num_states][num_v_heads][dv][dk], state_stride floats from one to the next */
+    void* out_dev;                           /* [n_tokens][num_v_heads][dv] in dtype */
+    const int32_t* starts_dev;               /* [num_sequences + 1] or null: one token each (n_tokens = num_sequences) */
+    const int32_t* slots_dev;                /* [num_sequences] or null: sequence i has state i */
+    const int32_t* fresh_dev;                /* [num_sequences] or null: none starts from zero */
+    int32_t* status_dev;                     /* int32[2] or null */
+    int64_t q_stride, k_stride, v_stride, out_stride;   /* elements between consecutive tokens */
+    int64_t gate_stride;                     /* floats between consecutive tokens of alpha and of beta (no alignment rule) */
+    int64_t state_stride;
+    int64_t n_tokens;
+    int32_t num_sequences, num_states, max_tokens;
+    int32_t num_heads, num_v_heads, dk, dv;
+    int32_t dtype;
+} onela_delta_rule_args;
+onela_status onela_delta_rule(const onela_delta_rule_args* args, void* stream);
+
+/* One token per row of logits, drawn with random numbers that the caller gives (the sampled counterpart of
+ * onela_select_beams).  With w_i = exp((x_i - max) / temperature) and the tokens ordered by (x descending, index ascending):
+ * kept are the first top_k tokens, of those the shortest leading run whose mass reaches top_p of theirs, and of those the
+ * ones with w_i >= min_p; the largest is always kept.  The token is the first one, in the order of indices, at which the running sum of kept
+ * masses exceeds uniform * (sum of kept masses).  logprob = log(w / sum of kept masses) of that token.
+ * Masses are integers of at least 43 binary places below the largest one's, so the result does not depend on any order of additions.
+ * temperature <= 0 or NaN: the largest, lowest index on ties.  top_k < 1 or beyond the vocabulary, top_p >= 1 or NaN and
+ * min_p <= 0 or NaN: no such filter; top_p <= 0: the largest alone.  NaN logits count as -inf, which is never drawn; where the largest is
+ * +inf only those are kept; -0 equals +0.  A uniform outside [0, 1) is taken as the nearer end, NaN as 0.  A row that has nothing above -inf gets token -1 and
+ * logprob -inf.  vocab up to 360 000, else ONELA_E_CAPACITY. */
+typedef struct onela_sample_args {
+    const void* logits_dev;                  /* [rows][vocab] in dtype, logits_stride elements from row to row (any) */
+    const float *uniforms_dev;               /* [rows] */
+    const float *temperature_dev, *top_p_dev, *min_p_dev;   /* [rows] or null: 1, off, off */
+    const int32_t* top_k_dev;                /* [rows] or null: off */
+    int32_t* tokens_out_dev;                 /* [rows] */
+    float* logprobs_out_dev;                 /* [rows] or null */
+    int64_t logits_stride;
+    int32_t rows, vocab;
+    int32_t dtype;
+} onela_sample_args;
+onela_status onela_sample_tokens(const onela_sample_args* args, void* stream);
+
 const char* onela_status_string(onela_status s);
 
 #ifdef __cplusplus

@@ -12,8 +12,9 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import sysconfig
-from ctypes import POINTER, c_char_p, c_int32, c_int64, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from pathlib import Path
 
 import torch
@@ -30,6 +31,7 @@ def pycall_path() -> Path:
 
 OK, E_INVAL, E_CAPACITY, E_ORDER, E_CUDA, E_UNSUPPORTED, E_DEVICE_CHECK, E_TIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
 DTYPE_F32, DTYPE_BF16 = 0, 1
+NORM_NONE, NORM_L2, NORM_RMS = 0, 1, 2
 MAX_BATCH = 64
 FLAG_DRY_RUN, FLAG_FORCE_GENERIC, FLAG_GTR_DELTA, FLAG_SHARED_CHAINS = 1, 2, 4, 8
 
@@ -46,6 +48,24 @@ class OnelaConfig(ctypes.Structure):
     def value_heads(self) -> int:
         """Value heads: num_v_heads, or num_heads when that is 0 (one value head per key head)."""
         return self.num_v_heads or self.num_heads
+
+
+class NormRotateArgs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "positions", "inv_freq")] + \
+               [(n, c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride", "n_tokens")] + \
+               [(n, c_int32) for n in ("num_q_heads", "num_k_heads", "head_dim", "rotary_dim", "interleaved", "norm", "dtype")] + \
+               [("eps", c_float), ("q_scale", c_float)]
+
+
+class DeltaRuleArgs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "alpha", "beta", "states", "out", "starts", "slots", "fresh", "status")] + \
+               [(n, c_int64) for n in ("q_stride", "k_stride", "v_stride", "out_stride", "gate_stride", "state_stride", "n_tokens")] + \
+               [(n, c_int32) for n in ("num_sequences", "num_states", "max_tokens", "num_heads", "num_v_heads", "dk", "dv", "dtype")]
+
+
+class SampleArgs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("logits", "uniforms", "temperature", "top_p", "min_p", "top_k", "tokens_out", "logprobs_out")] + \
+               [("logits_stride", c_int64)] + [(n, c_int32) for n in ("rows", "vocab", "dtype")]
 
 
 class OnelaError(RuntimeError):
@@ -86,6 +106,9 @@ PROTOTYPES = {
     "onela_launch_count": (c_int64, [c_void_p]),
     "onela_uses_tensor_core_path": (c_int32, [c_void_p]),
     "onela_status_string": (c_char_p, [c_int32]),
+    "onela_norm_rotate": (c_int32, [POINTER(NormRotateArgs), c_void_p]),
+    "onela_delta_rule": (c_int32, [POINTER(DeltaRuleArgs), c_void_p]),
+    "onela_sample_tokens": (c_int32, [POINTER(SampleArgs), c_void_p]),
 }
 
 
@@ -164,6 +187,121 @@ def onela_select_beams_static(beam_scores, cand_logp, W_new, parents_out, codes_
     _check(load_library().onela_select_beams_static(
         c_void_p(beam_scores.data_ptr()), c_void_p(cand_logp.data_ptr()), R, W_prev, C, W_new, c_void_p(parents_out.data_ptr()),
         c_void_p(codes_out.data_ptr()), c_void_p(scores_out.data_ptr()), c_void_p(_stream_ptr(stream))), "onela_select_beams_static")
+
+
+# --- the operators around the beam decode (no context, no workspace; see onela.h) ---
+_NORM_CODE = {None: NORM_NONE, "none": NORM_NONE, "l2": NORM_L2, "rms": NORM_RMS}
+
+
+def _tensor(t, name, dtype, shape, device):
+    """t's address, after its device, type and shape (None: any extent) have been looked at; only its first dimension may be strided."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.device != device or device.type != "cuda":
+        raise ValueError(f"{name}: must live on the CUDA device of the call's other tensors, got {t.device} and {device}")
+    if t.dtype != dtype or t.dim() != len(shape) or any(e is not None and e != g for e, g in zip(shape, t.shape)):
+        raise ValueError(f"{name}: expected {dtype} of shape {tuple('any' if e is None else e for e in shape)}, got {t.dtype} {tuple(t.shape)}")
+    run = 1
+    for d in range(t.dim() - 1, 0, -1):
+        if t.shape[d] != 1 and t.stride(d) != run and t.numel():
+            raise ValueError(f"{name}: only the first dimension may be strided, got strides {t.stride()} for {tuple(t.shape)}")
+        run *= t.shape[d]
+    return t.data_ptr()
+
+
+def _row_stride(t) -> int:
+    """Elements between consecutive rows; for a single row (whose stride means nothing) the next allowed one."""
+    extent = math.prod(t.shape[1:])
+    if t.shape[0] <= 1:
+        per = max(1, 16 // t.element_size())
+        return (extent + per - 1) // per * per
+    return t.stride(0)
+
+
+def _dense(t, name, dtype, shape, device):
+    if t is None:
+        return None
+    p = _tensor(t, name, dtype, shape, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor, got strides {t.stride()}")
+    return p
+
+
+def _call(name, args, device, stream):
+    with torch.cuda.device(device):
+        _check(getattr(load_library(), name)(ctypes.byref(args), c_void_p(_stream_ptr(stream))), name)
+
+
+def _rec_dtype(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+    return t.dtype
+
+
+def onela_norm_rotate(q, k, q_out, k_out, norm="l2", eps=1e-6, q_scale=1.0, q_weight=None, k_weight=None, positions=None, inv_freq=None,
+                      interleaved=False, stream=None) -> None:
+    """Norms of queries and keys per head with the rotation by position (see onela.h).  q [N, Hq, d], k [N, Hk, d], bf16 or fp32, tokens
+    may be strided (slices of one projection); q_out and k_out take the results and may be q and k.  norm: "l2", "rms" (weights [d]
+    fp32, optional) or None.  positions int32 [N] and inv_freq fp32 [r / 2] turn the first r elements of each head."""
+    dt, dev = _rec_dtype(q, "q"), q.device
+    if q.dim() != 3:
+        raise ValueError(f"q: expected [tokens, heads, d], got {tuple(q.shape)}")
+    if norm not in _NORM_CODE:
+        raise ValueError(f"norm: expected 'l2', 'rms' or None, got {norm!r}")
+    if (positions is None) != (inv_freq is None):
+        raise ValueError("positions and inv_freq go together")
+    if norm != "rms" and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights go with norm='rms'")
+    n, hq, d = q.shape
+    a = NormRotateArgs(q=_tensor(q, "q", dt, (n, hq, d), dev), k=_tensor(k, "k", dt, (n, None, d), dev), q_out=_tensor(q_out, "q_out", dt, (n, hq, d), dev),
+                       k_out=_tensor(k_out, "k_out", dt, tuple(k.shape), dev), q_weight=_dense(q_weight, "q_weight", torch.float32, (d,), dev),
+                       k_weight=_dense(k_weight, "k_weight", torch.float32, (d,), dev), positions=_dense(positions, "positions", torch.int32, (n,), dev),
+                       inv_freq=_dense(inv_freq, "inv_freq", torch.float32, (None,), dev), q_stride=_row_stride(q), k_stride=_row_stride(k),
+                       q_out_stride=_row_stride(q_out), k_out_stride=_row_stride(k_out), n_tokens=n, num_q_heads=hq, num_k_heads=k.shape[1], head_dim=d,
+                       rotary_dim=0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved=bool(interleaved), norm=_NORM_CODE[norm], dtype=_DTYPE_CODE[dt],
+                       eps=eps, q_scale=q_scale)
+    _call("onela_norm_rotate", a, dev, stream)
+
+
+def onela_delta_rule(q, k, v, alpha, beta, states, out, starts=None, slots=None, fresh=None, max_tokens=0, status=None, stream=None) -> None:
+    """The gated delta rule over ragged sequences (see onela.h).  q, k [N, H, dk], v and out [N, Hv, dv], bf16 or fp32; alpha, beta [N, Hv]
+    fp32; states [slots, Hv, dv, dk] fp32, updated in place; all may be strided in their first dimension.  starts int32 [n + 1] (None: one token
+    per sequence), slots int32 [n] (None: sequence i has state i; negative: padding), fresh int32 [n] (not 0: from the zero state), status int32
+    [2] or None.  max_tokens: the longest sequence that is expected."""
+    dt, dev, f32, i32 = _rec_dtype(q, "q"), q.device, torch.float32, torch.int32
+    if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
+        raise ValueError("q, v: expected [tokens, heads, d]")
+    (N, H, dk), (_, Hv, dv) = q.shape, v.shape
+    n = N if starts is None else starts.shape[0] - 1
+    if n < 0:
+        raise ValueError("starts: expected at least one entry")
+    a = DeltaRuleArgs(q=_tensor(q, "q", dt, (N, H, dk), dev), k=_tensor(k, "k", dt, (N, H, dk), dev), v=_tensor(v, "v", dt, (N, Hv, dv), dev),
+                      alpha=_tensor(alpha, "alpha", f32, (N, Hv), dev), beta=_tensor(beta, "beta", f32, (N, Hv), dev),
+                      states=_tensor(states, "states", f32, (None, Hv, dv, dk), dev), out=_tensor(out, "out", dt, (N, Hv, dv), dev),
+                      starts=_dense(starts, "starts", i32, (n + 1,), dev), slots=_dense(slots, "slots", i32, (n,), dev), fresh=_dense(fresh, "fresh", i32, (n,), dev),
+                      status=_dense(status, "status", i32, (2,), dev), q_stride=_row_stride(q), k_stride=_row_stride(k), v_stride=_row_stride(v),
+                      out_stride=_row_stride(out), gate_stride=_row_stride(alpha), state_stride=_row_stride(states), n_tokens=N, num_sequences=n,
+                      num_states=states.shape[0], max_tokens=max_tokens, num_heads=H, num_v_heads=Hv, dk=dk, dv=dv, dtype=_DTYPE_CODE[dt])
+    if N > 1 and alpha.stride(0) != beta.stride(0):
+        raise ValueError(f"alpha, beta: expected the same strides, got {alpha.stride()} and {beta.stride()}")
+    _call("onela_delta_rule", a, dev, stream)
+
+
+def onela_sample_tokens(logits, uniforms, tokens_out, temperature=None, top_k=None, top_p=None, min_p=None, logprobs_out=None, stream=None) -> None:
+    """One token per row of logits [R, V] (bf16 or fp32, rows may be strided) from uniforms fp32 [R] into tokens_out int32 [R] (see onela.h).
+    temperature, top_p, min_p fp32 [R], top_k int32 [R]: None where not wanted; logprobs_out fp32 [R] or None."""
+    dt, dev, f32 = _rec_dtype(logits, "logits"), logits.device, torch.float32
+    if logits.dim() != 2:
+        raise ValueError(f"logits: expected [rows, vocabulary], got {tuple(logits.shape)}")
+    R, V = logits.shape
+    a = SampleArgs(logits=_tensor(logits, "logits", dt, (R, V), dev),
+                   uniforms=_dense(uniforms, "uniforms", f32, (R,), dev), temperature=_dense(temperature, "temperature", f32, (R,), dev),
+                   top_p=_dense(top_p, "top_p", f32, (R,), dev), min_p=_dense(min_p, "min_p", f32, (R,), dev), top_k=_dense(top_k, "top_k", torch.int32, (R,), dev),
+                   tokens_out=_dense(tokens_out, "tokens_out", torch.int32, (R,), dev), logprobs_out=_dense(logprobs_out, "logprobs_out", f32, (R,), dev),
+                   logits_stride=logits.stride(0) if R > 1 else V, rows=R, vocab=V, dtype=_DTYPE_CODE[dt])
+    _call("onela_sample_tokens", a, dev, stream)
 
 
 def onela_workspace_bytes(cfg: OnelaConfig) -> int:
