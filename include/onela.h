@@ -314,7 +314,8 @@ onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream)
  * States, outputs and inputs do not overlap.
  * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it
  * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores.
- * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED. */
+ * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED.
+ * At most 65 535 sequences and 2^31 - 256 tokens, else ONELA_E_CAPACITY. */
 typedef struct onela_delta_rule_args {
     const void *q_dev, *k_dev, *v_dev;       /* [n_tokens][num_heads][dk] twice, [n_tokens][num_v_heads][dv] in dtype */
     const float *alpha_dev, *beta_dev;       /* [n_tokens][num_v_heads] */

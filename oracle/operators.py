@@ -36,9 +36,10 @@ def norm_rotate(x, norm, eps, scale=1.0, weight=None, positions=None, inv_freq=N
     return y * scale
 
 
-def delta_rule(q, k, v, alpha, beta, states, ranges, slots, fresh):
+def delta_rule(q, k, v, alpha, beta, states, ranges, slots, fresh, trace=None):
     """q, k [N, H, dk], v [N, Hv, dv], alpha, beta [N, Hv], states [slots, Hv, dv, dk]; ranges: (first row, one behind the last) per
-    sequence; slots[i] < 0: padded.  Returns (out {row: [Hv, dv]}, states), fp64."""
+    sequence; slots[i] < 0: padded.  Returns (out {row: [Hv, dv]}, states), fp64.  trace, a dict: gets per row the norms [Hv] of the state before
+    it and of its update vector."""
     q, k, v, alpha, beta = (np.asarray(x, dtype=np.float64) for x in (q, k, v, alpha, beta))
     states = np.array(states, dtype=np.float64)
     g = v.shape[1] // k.shape[1]
@@ -49,8 +50,11 @@ def delta_rule(q, k, v, alpha, beta, states, ranges, slots, fresh):
         S = np.zeros_like(states[slots[i]]) if fresh[i] else states[slots[i]].copy()
         for t in range(a, b):
             kt, qt = np.repeat(k[t], g, axis=0), np.repeat(q[t], g, axis=0)
+            before = np.sqrt((S * S).sum((1, 2)))
             S = S * alpha[t][:, None, None]
             d = beta[t][:, None] * (v[t] - np.einsum("hvk,hk->hv", S, kt))
+            if trace is not None:
+                trace[t] = (before, np.sqrt((d * d).sum(1)))
             S = S + d[:, :, None] * kt[:, None, :]
             out[t] = np.einsum("hvk,hk->hv", S, qt)
         states[slots[i]] = S

@@ -19,6 +19,7 @@ namespace onela {
 namespace {
 
 constexpr int WARPS = 4;
+constexpr int CHUNKED_FROM = 32;          // tokens of the longest sequence from which the chunked kernel is the faster one
 
 template <typename T>
 __device__ __forceinline__ void load4(const T* p, float* x);
@@ -174,7 +175,7 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
     if (g->num_v_heads % g->num_heads != 0 || g->num_v_heads > 65535) return ONELA_E_INVAL;
     if (g->dk != 32 && g->dk != 64 && g->dk != 128 && g->dk != 256) return ONELA_E_UNSUPPORTED;
     if (g->dv < 32 || g->dv % 32 != 0 || g->dv > 512) return ONELA_E_UNSUPPORTED;
-    if (g->num_sequences > 65535 || g->n_tokens > 0x7fffffffll) return ONELA_E_CAPACITY;
+    if (g->num_sequences > 65535 || g->n_tokens > 0x7fffff00ll) return ONELA_E_CAPACITY;
     if (!g->starts_dev && g->n_tokens != g->num_sequences) return ONELA_E_INVAL;
     if (!g->slots_dev && g->num_states < g->num_sequences) return ONELA_E_INVAL;
     if (g->num_sequences == 0 || g->num_states == 0) return ONELA_OK;
@@ -193,6 +194,8 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
                       g->q_stride, g->k_stride, g->v_stride, g->out_stride, g->gate_stride, g->state_stride, g->n_tokens,
                       g->num_sequences, g->num_states, g->num_heads, g->num_v_heads, g->dv, g->dk};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = g->dtype == ONELA_DTYPE_BF16 ? launch_step_t<__nv_bfloat16>(a, s) : launch_step_t<float>(a, s);
+    const long long longest = !g->starts_dev ? 1 : g->max_tokens > 0 ? g->max_tokens : g->n_tokens;
+    const cudaError_t e = longest >= CHUNKED_FROM && delta_chunk_supported(g->dk, g->dv) ? launch_delta_chunk(a, g->dtype, s)
+                          : g->dtype == ONELA_DTYPE_BF16 ? launch_step_t<__nv_bfloat16>(a, s) : launch_step_t<float>(a, s);
     return e == cudaSuccess ? ONELA_OK : ONELA_E_CUDA;
 }

@@ -1,0 +1,765 @@
+// The gated delta rule over long sequences, in chunks of C = 64 tokens on the tensor cores (sm_100a): outputs of every token and the
+// state behind the last (onela_delta_rule; token by token: onela_delta.cu).  dk in {32, 64, 128}, any dv.
+//
+// With g_i = prod_{l <= i} alpha_l inside the chunk, A_ij = beta_i (g_i / g_j)(k_i . k_j) for j < i and T = (I + A)^-1 (unit lower
+// triangular; ratios are running products, nothing is divided), Eq. 1 over the chunk is (WY form of a product of Householder-like
+// factors, Bischof and Van Loan 1987; with gates, Gated DeltaNet, Yang et al. 2024)
+//      Z = S K^T ,  X = (V^T - Z diag(g)) diag(beta) ,  D = X T^T                         (dv x C: column i is delta_i)
+//      O = S Q^T diag(g) + D P^T ,  P_ij = (g_i / g_j)(q_i . k_j) for j <= i              (dv x C)
+//      S <- g_C S + D diag(g_C / g) K .
+// T is applied to X, inside the chain, and not to K and V ahead of it: that costs the chain a product of 128 x 64 x 64, and
+// spares the preparation two products of that size with their operands and read-backs (in onela_prefill.cu the preparation is what
+// binds), and the memory of their tiles, where the queries find room.
+//
+// One CTA = (128 rows of the state, value head, sequence), all chunks of the sequence in order.  The state's rows lie in registers, a row in
+// two threads (a half each), which are in the two CHAIN warpgroups; all products have the rows as M = 128 lanes:
+//      S [K; Q]^T       one MMA set for Z and S Q^T (N = 128; the low half of S for Z alone where outputs are bf16)
+//      X T^T, D K, D P^T
+// PREPARING warpgroups take the chunks in turn: keys and queries to an operand tile (128 rows: 64 of K, 64 of Q), [K; Q] K^T in one MMA set,
+// A's and P's rows from it, T by blocks of 16 and joins, T and P as operand tiles.  An OUTPUT warpgroup brings the values into
+// shared memory and forms and stores O from the two accumulators, beside the chain's next steps.  All of it is coupled by mbarriers over rings.
+//
+// Precision.  S, X, D and the results are fp32; operands are sums of two fp16 numbers (22 to 23 significant bits) but for keys and queries
+// in bf16, which one fp16 number holds exactly, and for what only bf16 outputs see (S and D in their products with the queries' side, P): one fp16 number,
+// 2^-12 relative, a sixteenth of the outputs' own rounding.  Every operand row has its own power of two.
+//
+// Every wait is bounded: a thread that gives up raises the abort flag and keeps meeting its team's barriers, whose OR makes the team leave
+// together; ONELA_E_TIMEOUT goes to the caller's status word, if there is one.  Every MMA that was issued is waited for before tensor memory is freed.
+#include <algorithm>
+#include <mutex>
+
+#include "onela_chunk.cuh"
+#include "onela_delta.cuh"
+#include "onela_layout.cuh"
+#include "onela_sm100.cuh"
+
+namespace onela {
+namespace {
+
+using namespace chunk;
+using sm100::bar_or;
+using sm100::idesc_f16;
+using sm100::mbar_init;
+using sm100::mma_commit;
+using sm100::mma_ss;
+using sm100::mma_ts;
+using sm100::pow2_scale;
+using sm100::tmem_ld16;
+using sm100::tmem_st8;
+using sm100::umma_desc;
+
+constexpr int ROWS = 128;                 // state rows per CTA
+constexpr int KQ_BLOCK = 2 * TILE;        // 128 rows (64 of K, 64 of Q) of 64 fp16
+constexpr int NARROW = 3, WIDE = 12;      // largest elements of operand rows: K, Q, T, P in [2^3, 2^4), S, X, D in [2^12, 2^13)
+constexpr int CHAIN_BARRIER = 3;          // named barrier (1, 2: the preparing teams')
+
+template <int D, typename T>
+struct Shape {
+    static constexpr bool WIDE_T = sizeof(T) == 4;
+    static constexpr int KB = D > 64 ? D / 64 : 1;                 // K blocks of 64 elements
+    static constexpr int PARTS = WIDE_T ? 2 : 1;                   // fp16 parts of a key, a query, P
+    static constexpr int PREPS = WIDE_T && D == 128 ? 1 : 2;       // preparing teams
+    static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = WIDE_T ? 1 : 2;
+    static constexpr int PREP_THREADS = 128 * PREPS, CHAIN_THREADS = 256, THREADS = PREP_THREADS + CHAIN_THREADS + 128;
+    static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK, T_BYTES = 2 * TILE, P_BYTES = PARTS * TILE;
+    static constexpr int V_BYTES = C * ROWS * (int)sizeof(T);
+    static constexpr int A_BYTES = (C * AP * 4 + 1023) / 1024 * 1024, X_BYTES = 5 * 1024;
+    // per K stage: g / key scale, g / query scale, beta, g_C; per T stage: weights of D for the state, of D, of P's rows
+    static constexpr int KCO = 3 * C + 4, TCO = 3 * C;
+    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + 10 * ROWS) * 4 + 256;
+    static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
+    static_assert(SMEM <= 232448, "shared memory");
+    // tensor memory: S operand / D K | Z, X operand, D operand for the outputs (64) ; S Q^T (64) | D (64) | D P^T (64) | per preparing team 64
+    static constexpr uint32_t Z_COL = 128, O1_COL = Z_COL + C, D_COL = 256, O2_COL = 320, PREP_COL = 384, TMEM_COLS = 512;
+    // registers: 640 threads start with 96 each; the chain's state rows take what the other roles leave
+    static constexpr bool SPLIT_REGS = THREADS == 640 && D == 128;
+    static constexpr int PREP_REGS = 80, CHAIN_REGS = 128, OUT_REGS = 64;
+    static_assert(!SPLIT_REGS || 2 * PREP_REGS + 2 * CHAIN_REGS + OUT_REGS <= 5 * 96, "a split beyond the launch's registers waits for ever");
+};
+
+template <int D, typename T>
+__global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(const DeltaArgs a) {
+    using Z = Shape<D, T>;
+    constexpr int KB = Z::KB, PARTS = Z::PARTS, KS = (D < 64 ? D : 64) / 16;        // K steps of 16 per block of 64
+    constexpr int JOIN = D == 128 ? 2 : 8;                                          // see rows8
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* t_ring = smem + Z::K_STAGES * Z::KQ_BYTES;
+    uint8_t* p_ring = t_ring + Z::T_STAGES * Z::T_BYTES;
+    uint8_t* prep_s = p_ring + Z::T_STAGES * Z::P_BYTES;                            // per preparing team: matrix, scratch
+    T* v_s = reinterpret_cast<T*>(prep_s + Z::PREPS * (Z::A_BYTES + Z::X_BYTES));   // [token][row]
+    float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);
+    float* tco_s = kco_s + Z::K_STAGES * Z::KCO;
+    float* tok_s = tco_s + Z::T_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
+    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [3][2][ROWS] largest of a half row: S, X, D
+    float* inv_s = max_s + 6 * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
+    uint64_t* bars = reinterpret_cast<uint64_t*>(inv_s + 4 * ROWS);
+    auto bar_k = [&](int i) { return smem_u32(bars + i % Z::K_STAGES); };           // keys, queries, their weights
+    auto bar_kfree = [&](int i) { return smem_u32(bars + 3 + i % Z::K_STAGES); };
+    // T and P: the barriers of even and odd chunks, however many tiles there are (a wait by parity does not tell a chunk's turn from the
+    // one after next, and a team that comes early would take the one before for its own)
+    auto bar_t = [&](int i) { return smem_u32(bars + 6 + (i & 1)); };
+    auto bar_tfree = [&](int i) { return smem_u32(bars + 8 + (i & 1)); };
+    auto k_turn = [](int i) { return (uint32_t)(i / Z::K_STAGES) & 1; };
+    auto t_turn = [](int i) { return (uint32_t)(i >> 1) & 1; };
+    const uint32_t bar_v = smem_u32(bars + 10), bar_vfree = smem_u32(bars + 11);    // values
+    const uint32_t bar_z = smem_u32(bars + 12), bar_d = smem_u32(bars + 13), bar_s = smem_u32(bars + 14), bar_o = smem_u32(bars + 15);      // MMA sets
+    const uint32_t bar_ofree = smem_u32(bars + 16);                                 // the outputs' accumulators read out
+    auto bar_prep = [&](int w) { return smem_u32(bars + 17 + w); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int hv = blockIdx.y, hk = hv / (a.Hv / a.Hk), row_base = blockIdx.x * ROWS;
+    const bool first_cta = blockIdx.x == 0 && hv == 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Sequence seq = read_sequence(a, blockIdx.z, first_cta);
+    if (!seq.live) return;                                                          // (the whole CTA)
+    if (__syncthreads_or(taken_before(a, blockIdx.z, seq, tid, Z::THREADS))) {
+        if (first_cta && tid == 0) report_taken(a, blockIdx.z);
+        return;
+    }
+    const int n = (seq.length + C - 1) / C;                                         // chunks
+    if (tid == 0) {
+        for (int s = 0; s < 3; ++s) {
+            mbar_init(smem_u32(bars + s), 128);                                     // the preparing threads
+            mbar_init(smem_u32(bars + 3 + s), 1 + 128);                             // the chain's commit, the output threads
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(bars + 6 + s), 128);
+            mbar_init(smem_u32(bars + 8 + s), 1 + 128);
+        }
+        mbar_init(bar_v, 128);
+        mbar_init(bar_vfree, 1);
+        mbar_init(bar_z, 1);
+        mbar_init(bar_d, 1);
+        mbar_init(bar_s, 1);
+        mbar_init(bar_o, 2);                                                        // the commit, and the chain's leader (scales of the rows)
+        mbar_init(bar_ofree, 128);
+        for (int w = 0; w < 2; ++w) mbar_init(bar_prep(w), 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(Z::TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    // (not before tensor memory is this CTA's: a dependent launch may hold some of it while it waits for this one)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    bool fail = false;
+    // MMAs complete by themselves: nobody gives up early and leaves them behind
+    auto wait_mma = [&](uint32_t bar, uint32_t parity) {
+        if (!sm100::mbar_wait(bar, parity)) {
+            fail = true;
+            *abort_flag = 1;
+        }
+    };
+    // what another role has to do: bounded, and given up as soon as a role has
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        for (int i = 0; i < sm100::WAIT_LIMIT; ++i) {
+            if (sm100::mbar_try_wait(bar, parity)) return;
+            if ((i & 63) == 63 && *abort_flag) break;
+        }
+        fail = true;
+        *abort_flag = 1;
+    };
+
+    if (warp < 4 * Z::PREPS) {
+        // =============================== PREPARATION ===============================
+        if constexpr (Z::SPLIT_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Z::PREP_REGS));
+        const int team = warp >> 2, w4 = warp & 3, pt = tid & 127;
+        float* A_s = reinterpret_cast<float*>(prep_s + team * (Z::A_BYTES + Z::X_BYTES));       // [C][AP]
+        float* X_s = A_s + Z::A_BYTES / 4;                                                      // [32][36]
+        float* scale_s = tok_s + team * (128 + 3 * C);
+        float *alpha_s = scale_s + 128, *behind_s = alpha_s + C, *total_s = behind_s + C;       // total_s: product of the gates of either warp
+        const uint32_t acc_at = tmem_base + Z::PREP_COL + team * C;
+        constexpr int VEC = Vec16<T>::N, CPR = D / VEC, LR = CPR < 8 ? CPR : 8;      // 16-byte chunks and lanes per row
+        constexpr int PASS_ROWS = 128 / LR, PASSES = 128 / PASS_ROWS, NC = CPR / LR;
+        constexpr int BATCH = PASSES * NC > 8 ? 8 / NC : PASSES;                     // passes whose loads are in flight together
+        const T* kp = static_cast<const T*>(a.k) + seq.begin * a.k_stride + (long long)hk * D;
+        const T* qp = static_cast<const T*>(a.q) + seq.begin * a.q_stride + (long long)hk * D;
+        auto gate_of = [&](const float* g, int t, float pad) { return t < seq.length ? __ldg(g + (seq.begin + t) * a.gate_stride + hv) : pad; };
+        float alpha_next = 1.f, beta_next = 0.f;
+        if (team < n && pt < C) {
+            alpha_next = gate_of(a.alpha, team * C + pt, 1.f);
+            beta_next = gate_of(a.beta, team * C + pt, 0.f);
+        }
+        uint32_t phase = 0;
+        for (int i = team; i < n; i += Z::PREPS) {
+            const int t0 = i * C;
+            uint8_t* KQ_s = smem + i % Z::K_STAGES * Z::KQ_BYTES;
+            float* kco = kco_s + i % Z::K_STAGES * Z::KCO;
+            if (i >= Z::K_STAGES) wait(bar_kfree(i), k_turn(i - Z::K_STAGES));
+            // keys (rows 0 - 63) and queries (64 - 127) as the K-major operand tile, every row with its own power of two; tokens
+            // beyond the sequence are zeros with alpha = 1, beta = 0: they change nothing
+            const int lr = pt % LR, row0 = pt / LR;
+#pragma unroll
+            for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
+                uint4 raw[BATCH][NC];
+#pragma unroll
+                for (int p = 0; p < BATCH; ++p) {
+                    const int row = (p0 + p) * PASS_ROWS + row0, t = t0 + (row & 63);
+                    const T* src = row < C ? kp + t * a.k_stride : qp + t * a.q_stride;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) raw[p][c] = t < seq.length ? __ldg(reinterpret_cast<const uint4*>(src) + c * LR + lr) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int p = 0; p < BATCH; ++p) {
+                    const int row = (p0 + p) * PASS_ROWS + row0;
+                    float x[NC * VEC], m = 0.f;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) Vec16<T>::unpack(raw[p][c], x + c * VEC);
+#pragma unroll
+                    for (int e = 0; e < NC * VEC; ++e) m = fmaxf(m, fabsf(x[e]));
+#pragma unroll
+                    for (int o = LR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    float sc, inv;
+                    pow2_scale(m, NARROW, sc, inv);
+                    if (lr == 0) scale_s[row] = inv;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        const int el = (c * LR + lr) * VEC;
+                        uint8_t* dst = KQ_s + (el >> 6) * KQ_BLOCK + row * 128 + ((((el & 63) >> 3) ^ (row & 7)) << 4) + (el & 7) * 2;
+                        const float* y = x + c * VEC;
+                        if constexpr (VEC == 8) {        // bf16: exact in one fp16 number
+                            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_f16x2(y[0] * sc, y[1] * sc), pack_f16x2(y[2] * sc, y[3] * sc),
+                                                                        pack_f16x2(y[4] * sc, y[5] * sc), pack_f16x2(y[6] * sc, y[7] * sc));
+                        } else {
+                            uint32_t hi[2], lo[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) split2(y[2 * e] * sc, y[2 * e + 1] * sc, hi[e], lo[e]);
+                            *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
+                            *reinterpret_cast<uint2*>(dst + KB * KQ_BLOCK) = make_uint2(lo[0], lo[1]);
+                        }
+                    }
+                }
+            }
+            // products of the gates: up to a token (g) and behind it
+            float g = alpha_next, behind = alpha_next;
+            const float beta = beta_next;
+            if (pt < C) {
+                alpha_s[pt] = alpha_next;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const float x = __shfl_up_sync(0xffffffffu, g, o), y = __shfl_down_sync(0xffffffffu, behind, o);
+                    if (lane >= o) g *= x;
+                    if (lane + o < 32) behind *= y;
+                }
+                if (lane == 0) total_s[w4] = behind;
+                behind = __shfl_down_sync(0xffffffffu, behind, 1);
+                if (lane == 31) behind = 1.f;
+                if (i + Z::PREPS < n) {
+                    alpha_next = gate_of(a.alpha, t0 + Z::PREPS * C + pt, 1.f);
+                    beta_next = gate_of(a.beta, t0 + Z::PREPS * C + pt, 0.f);
+                }
+            }
+            proxy_fence();
+            tc_fence_before();
+            if (bar_or(1 + team, 128, fail ? 1 : 0)) { fail = true; break; }
+            if (w4 == 0) {          // [K; Q] K^T
+                tc_fence_after();
+                const uint64_t kd = umma_desc(smem_u32(KQ_s));
+#pragma unroll 1
+                for (int t = PARTS > 1 ? 2 : 0; t >= 0; --t)                // small terms first: (lo hi, hi lo,) hi hi
+#pragma unroll 1
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const int at = (kb * KQ_BLOCK + ks * 32) >> 4, low = (KB * KQ_BLOCK) >> 4;
+                            mma_ss(acc_at, kd + (at + (t == 2 ? low : 0)), kd + (at + (t == 1 ? low : 0)), idesc_f16(C), t != (PARTS > 1 ? 2 : 0) || kb || ks);
+                        }
+                mma_commit(bar_prep(team));
+            }
+            if (pt < C) {
+                if (w4 == 1) g *= total_s[0];
+                else behind *= total_s[1];
+                kco[pt] = g * scale_s[pt];
+                kco[C + pt] = g * scale_s[C + pt];
+                kco[2 * C + pt] = beta;
+                if (pt == C - 1) kco[3 * C] = g;
+                behind_s[pt] = behind * scale_s[pt];                            // (and what undoes the key's scale)
+            }
+            arrive(bar_k(i));
+            if (i + Z::PREPS < n) { // the lines of the team's next chunk into L2
+                constexpr int LINES = D * (int)sizeof(T) / 128 > 0 ? D * (int)sizeof(T) / 128 : 1;
+                for (int x = pt; x < 2 * C * LINES; x += 128) {
+                    const int row = (x >> 1) / LINES, ln = (x >> 1) % LINES, t = min(t0 + Z::PREPS * C + row, seq.length - 1);
+                    const char* p = reinterpret_cast<const char*>((x & 1) ? qp + t * a.q_stride : kp + t * a.k_stride) + ln * 128;
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+                }
+            }
+            wait_mma(bar_prep(team), phase);
+            phase ^= 1;
+            tc_fence_after();
+            // A's row i by thread i, P's row i by thread 64 + i.  (g_i / g_l) runs from the right: the product of the gates behind l.
+            uint8_t *T_s = t_ring + i % Z::T_STAGES * Z::T_BYTES, *P_s = p_ring + i % Z::T_STAGES * Z::P_BYTES;
+            float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
+            if (w4 < 2) {
+                const float coef = beta * scale_s[pt];
+                float ratio = 1.f;
+#pragma unroll 1
+                for (int cb = 3; cb >= 0; --cb) {
+                    uint32_t v[16];
+                    tmem_ld16(acc_at + cb * 16 + ((uint32_t)(w4 * 32) << 16), v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 12; e >= 0; e -= 4) {
+                        const float4 al = *reinterpret_cast<const float4*>(alpha_s + cb * 16 + e), ki = *reinterpret_cast<const float4*>(scale_s + cb * 16 + e);
+                        const float alv[4] = {al.x, al.y, al.z, al.w}, kiv[4] = {ki.x, ki.y, ki.z, ki.w};
+                        float row[4];
+#pragma unroll
+                        for (int f = 3; f >= 0; --f) {
+                            const int l = cb * 16 + e + f;
+                            row[f] = l < pt ? (coef * ratio) * (__uint_as_float(v[e + f]) * kiv[f]) : 0.f;
+                            ratio *= l <= pt ? alv[f] : 1.f;
+                        }
+                        *reinterpret_cast<float4*>(A_s + pt * AP + cb * 16 + e) = make_float4(row[0], row[1], row[2], row[3]);
+                    }
+                }
+                __syncwarp();
+                // T = (I + A)^-1 in place, from the diagonal out.  Blocks of 16, two per warp, one column per lane by forward
+                // substitution; then a warp's two blocks are joined, then the two warps': - T22 A21 T11 below the diagonal.
+                float* L = A_s + (w4 * 32) * (AP + 1) + (lane >> 4) * (16 * AP + 16);
+                const int col = lane & 15;
+                float x[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float s0 = r == col ? 1.f : 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int l = 0; l < r; l += 4) {
+                        const float4 q = *reinterpret_cast<const float4*>(L + r * AP + l);
+                        s0 = fmaf(-q.x, x[l], s0);
+                        if (l + 1 < r) s1 = fmaf(-q.y, x[l + 1], s1);
+                        if (l + 2 < r) s0 = fmaf(-q.z, x[l + 2], s0);
+                        if (l + 3 < r) s1 = fmaf(-q.w, x[l + 3], s1);
+                    }
+                    x[r] = s0 + s1;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int r = 0; r < 16; ++r) L[r * AP + col] = x[r];
+                __syncwarp();
+                float* B21 = A_s + (w4 * 32) * (AP + 1) + (16 + (lane >> 4) * 8) * AP;       // eight rows of the lower block per half warp
+                float acc[8];
+                rows8<16, JOIN>(acc, B21, A_s + (w4 * 32) * (AP + 1) + col, AP);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) X_s[w4 * (16 * 20) + ((lane >> 4) * 8 + r) * 20 + col] = acc[r];
+                __syncwarp();
+                rows8<16, JOIN>(acc, B21 + 16, X_s + w4 * (16 * 20) + col, 20);
+                __syncwarp();
+#pragma unroll
+                for (int r = 0; r < 8; ++r) B21[r * AP + col] = -acc[r];
+            } else {
+                const int me = pt - C;
+                const float coef = scale_s[pt];
+                float ratio = 1.f, m = 0.f, sc = 0.f, inv = 0.f;
+                if (i >= Z::T_STAGES) wait(bar_tfree(i - Z::T_STAGES), t_turn(i - Z::T_STAGES));
+                // once for the row's largest element, once for the operand
+#pragma unroll 1
+                for (int round = 0; round < 2; ++round) {
+                    if (round) {
+                        pow2_scale(m, NARROW, sc, inv);
+                        tco[2 * C + me] = inv;
+                        ratio = 1.f;
+                    }
+#pragma unroll 1
+                    for (int cb = 3; cb >= 0; --cb) {
+                        uint32_t v[16], hi[8], lo[8];
+                        tmem_ld16(acc_at + cb * 16 + ((uint32_t)(w4 * 32) << 16), v);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 12; e >= 0; e -= 4) {
+                            const float4 al = *reinterpret_cast<const float4*>(alpha_s + cb * 16 + e), ki = *reinterpret_cast<const float4*>(scale_s + cb * 16 + e);
+                            const float alv[4] = {al.x, al.y, al.z, al.w}, kiv[4] = {ki.x, ki.y, ki.z, ki.w};
+#pragma unroll
+                            for (int f = 3; f >= 0; --f) {
+                                const int l = cb * 16 + e + f;
+                                const float x = l <= me ? (coef * ratio) * (__uint_as_float(v[e + f]) * kiv[f]) : 0.f;
+                                ratio *= l <= me ? alv[f] : 1.f;
+                                m = round ? m : fmaxf(m, fabsf(x));
+                                v[e + f] = __float_as_uint(x * sc);
+                            }
+                        }
+                        if (round) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                uint8_t* dst = P_s + me * 128 + (((2 * cb + e) ^ (me & 7)) << 4);
+                                *reinterpret_cast<uint4*>(dst) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+                                if constexpr (PARTS > 1) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
+                            }
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            bar_or(1 + team, 128, 0);
+            {
+                float acc[8];
+                rows8<32, JOIN>(acc, A_s + (32 + 8 * w4) * AP, A_s + lane, AP);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) X_s[(8 * w4 + r) * 36 + lane] = acc[r];
+                bar_or(1 + team, 128, 0);
+                rows8<32, JOIN>(acc, A_s + (32 + 8 * w4) * AP + 32, X_s + lane, 36);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) A_s[(32 + 8 * w4 + r) * AP + lane] = -acc[r];
+            }
+            if (i >= Z::T_STAGES) wait(bar_tfree(i - Z::T_STAGES), t_turn(i - Z::T_STAGES));
+            if (bar_or(1 + team, 128, fail ? 1 : 0)) { fail = true; break; }
+            // T as an operand tile (fp16 hi, lo): row pt / 2 by threads pt and pt + 1, columns 16 h .. and 32 + 16 h .. (conflict-free reads)
+            {
+                const int ti = pt >> 1, hf = pt & 1;
+                float t[32], m = 0.f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float4 x = *reinterpret_cast<const float4*>(A_s + ti * AP + 16 * hf + (q >> 2) * 32 + (q & 3) * 4);
+                    t[4 * q] = x.x; t[4 * q + 1] = x.y; t[4 * q + 2] = x.z; t[4 * q + 3] = x.w;
+                }
+                // (what lies above the diagonal is no part of T: the upper right quarter still holds A's zeros)
+#pragma unroll
+                for (int q = 0; q < 32; ++q) m = fmaxf(m, fabsf(t[q]));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                float sc, inv;
+                pow2_scale(m, NARROW, sc, inv);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {                               // chunks of eight columns
+                    const int ch = 4 * (c >> 1) + 2 * hf + (c & 1), at = ti * 128 + ((ch ^ (ti & 7)) << 4);
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) split2(t[8 * c + 2 * e] * sc, t[8 * c + 2 * e + 1] * sc, hi[e], lo[e]);
+                    *reinterpret_cast<uint4*>(T_s + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(T_s + TILE + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+                if (hf == 0) {
+                    tco[ti] = inv * behind_s[ti];
+                    tco[C + ti] = inv;
+                }
+            }
+            proxy_fence();
+            arrive(bar_t(i));
+        }
+    } else if (warp < 4 * Z::PREPS + 8) {
+        // =============================== STATE ROWS ===============================
+        if constexpr (Z::SPLIT_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Z::CHAIN_REGS));
+        constexpr int H = D / 2, HB = H / 16;                     // a thread's part of its row, in blocks of 16
+        const int c = (warp >> 2) - Z::PREPS, r = (warp & 3) * 32 + lane;
+        const bool is_row = row_base + r < a.dv;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem_base + lanes + c * H, z_at = tmem_base + lanes + Z::Z_COL + 32 * c, d_at = tmem_base + lanes + Z::D_COL + 32 * c;
+        const bool issuer = warp == 4 * Z::PREPS, leader = issuer && lane == 0;
+        float* mine = max_s + c * ROWS + r;                       // + 2 ROWS per kind
+        const float* other = max_s + (1 - c) * ROWS + r;
+        float* state = a.states + seq.slot * a.state_stride + ((long long)hv * a.dv + row_base + r) * D + c * H;
+        auto meet = [&] { return bar_or(CHAIN_BARRIER, Z::CHAIN_THREADS, fail ? 1 : 0); };
+        float S[H], m = 0.f;
+#pragma unroll
+        for (int e = 0; e < H; e += 4) {
+            const float4 x = is_row && !seq.fresh ? __ldcs(reinterpret_cast<const float4*>(state + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            S[e] = x.x; S[e + 1] = x.y; S[e + 2] = x.z; S[e + 3] = x.w;
+        }
+#pragma unroll
+        for (int e = 0; e < H; ++e) m = fmaxf(m, fabsf(S[e]));
+        *mine = m;
+        meet();
+        int issued = 0;                                           // chunks whose last products have been issued
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const uint32_t turn = i & 1;
+            const float* kco = kco_s + i % Z::K_STAGES * Z::KCO;
+            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
+            float sc, inv_row;
+            // ---- Z = S K^T, and S Q^T ----
+            pow2_scale(fmaxf(m, *other), WIDE, sc, inv_row);
+#pragma unroll
+            for (int b = 0; b < HB; ++b) split_to_tmem(s_at + 16 * b, S + 16 * b, sc);
+            if (c == 0) inv_s[turn * ROWS + r] = inv_row;
+            tc_wait_st();
+            tc_fence_before();
+            wait(bar_k(i), k_turn(i));
+            if (i > 0) wait(bar_ofree, turn ^ 1);
+            if (meet()) { fail = true; break; }
+            if (issuer) {
+                tc_fence_after();
+                const uint64_t kd = umma_desc(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES));
+                bool first = true;
+                auto product = [&](int sp, int kp, int cols) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const int kb = ks / KS;
+                        mma_ts(tmem_base + Z::Z_COL, tmem_base + ks * 16 + sp * 8, kd + ((((kp * KB + kb) * KQ_BLOCK) + (ks - kb * KS) * 32) >> 4), idesc_f16(cols), !first);
+                        first = false;
+                    }
+                };
+                if constexpr (PARTS > 1) {
+                    product(1, 0, 2 * C);
+                    product(0, 1, 2 * C);
+                    product(0, 0, 2 * C);
+                } else {
+                    product(0, 0, 2 * C);
+                    product(1, 0, C);
+                }
+                mma_commit(bar_z);
+            }
+            wait(bar_v, turn);
+            wait_mma(bar_z, turn);
+            tc_fence_after();
+            // ---- X = (V^T - Z diag(g)) diag(beta) ----
+            float x[32], mx = 0.f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t v[16];
+                tmem_ld16(z_at + 16 * b, v);
+                float val[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if constexpr (sizeof(T) == 2) val[e] = __bfloat162float(v_s[(32 * c + 16 * b + e) * ROWS + r]);
+                    else val[e] = v_s[(32 * c + 16 * b + e) * ROWS + r];
+                }
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 gz = *reinterpret_cast<const float4*>(kco + 32 * c + 16 * b + e), be = *reinterpret_cast<const float4*>(kco + 2 * C + 32 * c + 16 * b + e);
+                    const float gzv[4] = {gz.x, gz.y, gz.z, gz.w}, bev[4] = {be.x, be.y, be.z, be.w};
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const float y = bev[f] * fmaf(-gzv[f], __uint_as_float(v[e + f]) * inv_row, val[e + f]);
+                        x[16 * b + e + f] = y;
+                        mx = fmaxf(mx, fabsf(y));
+                    }
+                }
+            }
+            const float g_chunk = kco[3 * C];
+            mine[2 * ROWS] = mx;
+            if (meet()) { fail = true; break; }
+            if (leader) arrive(bar_vfree);
+            float inv_x;
+            pow2_scale(fmaxf(mx, other[2 * ROWS]), WIDE, sc, inv_x);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
+            tc_wait_st();
+            tc_fence_before();
+            wait(bar_t(i), t_turn(i));
+            if (meet()) { fail = true; break; }
+            // ---- D = X T^T ----
+            if (issuer) {
+                tc_fence_after();
+                const uint64_t td = umma_desc(smem_u32(t_ring + i % Z::T_STAGES * Z::T_BYTES));
+#pragma unroll
+                for (int t = 2; t >= 0; --t)                      // small terms first: lo hi, hi lo, hi hi
+#pragma unroll
+                    for (int ks = 0; ks < C / 16; ++ks)
+                        mma_ts(tmem_base + Z::D_COL, tmem_base + Z::Z_COL + ks * 16 + (t == 2 ? 8 : 0), td + (((t == 1 ? TILE : 0) + ks * 32) >> 4), idesc_f16(C), t != 2 || ks);
+                mma_commit(bar_d);
+            }
+            wait_mma(bar_d, turn);
+            tc_fence_after();
+            // ---- D's operands: times g_C / g (and what undoes the keys' scales) for the state, as it is for the outputs, one scale for both ----
+            float md = 0.f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t v[16];
+                tmem_ld16(d_at + 16 * b, v);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e), u = *reinterpret_cast<const float4*>(tco + C + 32 * c + 16 * b + e);
+                    const float wv[4] = {w.x, w.y, w.z, w.w}, uv[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const float y = __uint_as_float(v[e + f]) * inv_x;
+                        x[16 * b + e + f] = y;
+                        md = fmaxf(md, fmaxf(fabsf(y * wv[f]), fabsf(y * uv[f])));
+                    }
+                }
+            }
+            mine[4 * ROWS] = md;
+            if (meet()) { fail = true; break; }
+            float inv_d;
+            pow2_scale(fmaxf(md, other[4 * ROWS]), WIDE, sc, inv_d);
+            if (c == 0) inv_s[(2 + turn) * ROWS + r] = inv_d;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float y[16];
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 w4 = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
+                    y[e] = x[16 * b + e] * w4.x; y[e + 1] = x[16 * b + e + 1] * w4.y; y[e + 2] = x[16 * b + e + 2] * w4.z; y[e + 3] = x[16 * b + e + 3] * w4.w;
+                }
+                split16(y, sc, w, w + 8);
+                tmem_st16(d_at + 16 * b, w);
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 u4 = *reinterpret_cast<const float4*>(tco + C + 32 * c + 16 * b + e);
+                    y[e] = x[16 * b + e] * u4.x; y[e + 1] = x[16 * b + e + 1] * u4.y; y[e + 2] = x[16 * b + e + 2] * u4.z; y[e + 3] = x[16 * b + e + 3] * u4.w;
+                }
+                if constexpr (PARTS > 1) {
+                    split16(y, sc, w, w + 8);
+                    tmem_st16(z_at + 16 * b, w);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = pack_f16x2(y[2 * e] * sc, y[2 * e + 1] * sc);
+                    tmem_st8(z_at + 16 * b, w);
+                }
+            }
+            tc_wait_st();
+            tc_fence_before();
+            if (meet()) { fail = true; break; }
+            // ---- D K over the S operand (read by now), and D P^T ----
+            if (issuer) {
+                tc_fence_after();
+                const uint64_t kd = umma_desc_mn(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES), KQ_BLOCK);
+                const uint64_t pd = umma_desc(smem_u32(p_ring + i % Z::T_STAGES * Z::P_BYTES));
+                bool first = true;
+                auto product = [&](int dp, int kp) {
+#pragma unroll
+                    for (int ks = 0; ks < C / 16; ++ks) {
+                        mma_ts(tmem_base, tmem_base + Z::D_COL + ks * 16 + dp * 8, kd + ((kp * KB * KQ_BLOCK + ks * 2048) >> 4), idesc_f16(D) | B_MN_MAJOR, !first);
+                        first = false;
+                    }
+                };
+                if constexpr (PARTS > 1) product(0, 1);
+                product(1, 0);
+                product(0, 0);
+                mma_commit(bar_s);
+#pragma unroll
+                for (int t = PARTS > 1 ? 2 : 0; t >= 0; --t)
+#pragma unroll
+                    for (int ks = 0; ks < C / 16; ++ks)
+                        mma_ts(tmem_base + Z::O2_COL, tmem_base + Z::Z_COL + ks * 16 + (t == 2 ? 8 : 0), pd + (((t == 1 ? TILE : 0) + ks * 32) >> 4), idesc_f16(C),
+                               t != (PARTS > 1 ? 2 : 0) || ks);
+                mma_commit(bar_o);
+                mma_commit(bar_kfree(i));
+                mma_commit(bar_tfree(i));
+            }
+            if (leader) arrive(bar_o);
+            issued = i + 1;
+            wait_mma(bar_s, turn);
+            tc_fence_after();
+            m = 0.f;
+#pragma unroll
+            for (int b = 0; b < HB; ++b) {
+                uint32_t v[16];
+                tmem_ld16(s_at + 16 * b, v);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    S[16 * b + e] = fmaf(g_chunk, S[16 * b + e], __uint_as_float(v[e]) * inv_d);
+                    m = fmaxf(m, fabsf(S[16 * b + e]));
+                }
+            }
+            *mine = m;
+            tc_fence_before();
+            if (meet()) { fail = true; break; }
+        }
+        if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
+        if (!fail && is_row) {
+#pragma unroll
+            for (int e = 0; e < H; e += 4) __stcs(reinterpret_cast<float4*>(state + e), make_float4(S[e], S[e + 1], S[e + 2], S[e + 3]));
+        }
+    } else {
+        // =============================== VALUES IN, OUTPUTS OUT ===============================
+        if constexpr (Z::SPLIT_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Z::OUT_REGS));
+        const int ot = tid & 127, r = ot;
+        const bool is_row = row_base + r < a.dv;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int rows = min(ROWS, a.dv - row_base);              // a multiple of 32
+        const T* vp = static_cast<const T*>(a.v) + seq.begin * a.v_stride + (long long)hv * a.dv + row_base;
+        T* op = static_cast<T*>(a.out) + seq.begin * a.out_stride + (long long)hv * a.dv + row_base + r;
+        constexpr int VEC = Vec16<T>::N, CH = ROWS / VEC;         // 16-byte chunks per token
+        auto load_values = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < C * CH / 128; ++x) {
+                const int item = x * 128 + ot, t = item / CH, ch = item % CH, token = i * C + t;
+                const bool there = token < seq.length && ch * VEC < rows;
+                const uint32_t dst = smem_u32(v_s + t * ROWS + ch * VEC);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(there ? vp + token * a.v_stride + ch * VEC : vp), "r"(there ? 16 : 0) : "memory");
+            }
+            asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+            arrive(bar_v);
+        };
+        if (n > 0) load_values(0);
+#pragma unroll 1
+        for (int i = 0; i < n && !fail; ++i) {
+            const uint32_t turn = i & 1;
+            const float* kco = kco_s + i % Z::K_STAGES * Z::KCO + C;
+            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO + 2 * C;
+            if (i + 1 < n) {
+                wait(bar_vfree, turn);
+                if (!fail) load_values(i + 1);
+            }
+            wait(bar_o, turn);
+            // (the warps of this team do not wait for one another; a warp's threads leave together)
+            if (__any_sync(0xffffffffu, fail)) { fail = true; break; }
+            tc_fence_after();
+            const float inv_row = inv_s[turn * ROWS + r], inv_d = inv_s[(2 + turn) * ROWS + r];
+#pragma unroll 1
+            for (int b = 0; b < 4; ++b) {
+                uint32_t v[16], w[16];
+                tmem_ld16(tmem_base + lanes + Z::O1_COL + 16 * b, v);
+                tmem_ld16(tmem_base + lanes + Z::O2_COL + 16 * b, w);
+                tc_wait_ld();
+                if (b == 3) {
+                    tc_fence_before();
+                    arrive(bar_ofree);
+                }
+                T* dst = op + (long long)(i * C + 16 * b) * a.out_stride;
+                const int left = seq.length - (i * C + 16 * b);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float o = fmaf(__uint_as_float(v[e]) * inv_row, kco[16 * b + e], __uint_as_float(w[e]) * inv_d * tco[16 * b + e]);
+                    if (is_row && e < left) {
+                        if constexpr (sizeof(T) == 2) dst[e * a.out_stride] = __float2bfloat16_rn(o);
+                        else dst[e * a.out_stride] = o;
+                    }
+                }
+            }
+            arrive(bar_kfree(i));
+            arrive(bar_tfree(i));
+        }
+    }
+    if (fail && a.status && atomicCAS(a.status, ONELA_OK, ONELA_E_TIMEOUT) == ONELA_OK) a.status[1] = blockIdx.z;
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(Z::TMEM_COLS) : "memory");
+}
+
+template <int D, typename T>
+cudaError_t launch_dt(const DeltaArgs& a, cudaStream_t stream) {
+    using Z = Shape<D, T>;
+    auto kern = delta_chunk_kernel<D, T>;
+    constexpr int MAX_DEVICES = 64;
+    static std::mutex setup_mutex;
+    static bool ready[MAX_DEVICES] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(setup_mutex);
+        if (!ready[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Z::SMEM);
+            if (e != cudaSuccess) return e;
+            ready[dev] = true;
+        }
+    }
+    return launch_dependent(kern, dim3((a.dv + ROWS - 1) / ROWS, a.Hv, a.num_sequences), dim3(Z::THREADS), Z::SMEM, stream, a);
+}
+template <int D>
+cudaError_t launch_d(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
+    return dtype == ONELA_DTYPE_BF16 ? launch_dt<D, __nv_bfloat16>(a, stream) : launch_dt<D, float>(a, stream);
+}
+
+}  // namespace
+
+bool delta_chunk_supported(int32_t dk, int32_t) { return dk == 32 || dk == 64 || dk == 128; }
+
+cudaError_t launch_delta_chunk(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
+    return a.dk == 32 ? launch_d<32>(a, dtype, stream) : a.dk == 64 ? launch_d<64>(a, dtype, stream) : launch_d<128>(a, dtype, stream);
+}
+
+}  // namespace onela

@@ -4,7 +4,12 @@ grouped heads, padding, fresh sequences, strides, bad slots and ranges.
 Tolerance, relative to the 2-norm of the vector (an output) or matrix (a state): 2^-24 times 16 roundings per token - a row's dot product takes 16 / 2
 in a lane and up to 4 across lanes, delta, decay and update four more - for the tokens that the state still remembers, at most 20 at gates in [0.9, 1]; outputs
 add half a step of their type per element.  The chunked form (operands in two fp16 parts: 2^-22 per product, three products in a
-chunk of 64 tokens) stays below that."""
+chunk of 64 tokens) stays below that.
+
+bf16 outputs of the chunked form come from S Q^T + D P^T with S (the state before the chunk), D (the chunk's update vectors) and P (weights
+(g_i / g_j) q_i . k_j) rounded to fp16: every factor is off by up to 2^-11 of itself, evenly, so by 2^-11 / sqrt(3) in the mean square, independently.  The error's
+mean square is then (2^-22 / 3) times the sum of the terms' squares, |S|^2 |q|^2 / dk + 2 sum_j (q . k_j)^2 |d_j|^2 over the chunk's tokens up to this
+one (gates at most 1); three standard deviations are allowed."""
 import numpy as np
 import pytest
 import torch
@@ -42,17 +47,30 @@ class Batch:
         return torch.tensor(x, dtype=torch.int32, device="cuda")
 
     def run(self, max_tokens=0, stream=None, **over):
+        self.chunked = (max_tokens or self.q.shape[0]) >= 32
         kw = over or dict(starts=self.starts, slots=self.i32(self.slots), fresh=self.i32(self.fresh), status=self.status)
         P.onela_delta_rule(self.q, self.k, self.v, self.alpha, self.beta, self.states, self.out, stream=stream, max_tokens=max_tokens, **kw)
 
     def reference(self, live=None):
         c = lambda x: x.double().cpu().numpy()  # noqa: E731
         slots = [s if live is None or live[i] else -1 for i, s in enumerate(self.slots)]
-        return plain.delta_rule(c(self.q), c(self.k), c(self.v), c(self.alpha), c(self.beta), c(self.states), self.ranges, slots, self.fresh), slots
+        self.trace = {}
+        return plain.delta_rule(c(self.q), c(self.k), c(self.v), c(self.alpha), c(self.beta), c(self.states), self.ranges, slots, self.fresh, self.trace), slots
 
     def check(self, ref, slots, memory=20):
         (out, states), got, got_s = ref, self.out.double().cpu().numpy(), self.states.double().cpu().numpy()
         half = torch.finfo(DT[self.dtype]).eps / 2
+        q, k = self.q.double().cpu().numpy(), self.k.double().cpu().numpy()
+        g = got.shape[1] // q.shape[1]
+
+        def rounding(a, t, h):           # of bf16 outputs in the chunked form
+            if self.dtype != "bf16" or not self.chunked:
+                return 0.0
+            first = a + (t - a) // 64 * 64
+            dots = (q[t, h // g] * k[first:t + 1, h // g]).sum(-1)
+            deltas = np.array([self.trace[j][1][h] for j in range(first, t + 1)])
+            terms = self.trace[first][0][h] ** 2 * (q[t, h // g] ** 2).sum() / q.shape[-1] + 2 * (dots ** 2 * deltas ** 2).sum()
+            return 3 * 2.0 ** -11 / np.sqrt(3) * np.sqrt(terms)
         for i, (a, b) in enumerate(self.ranges):
             if slots[i] < 0:
                 continue
@@ -60,7 +78,7 @@ class Batch:
             for t in range(a, b):
                 for h in range(got.shape[1]):
                     err = np.maximum(np.abs(got[t, h] - out[t][h]) - half * np.abs(out[t][h]), 0)
-                    assert np.linalg.norm(err) <= tol * max(np.linalg.norm(out[t][h]), np.linalg.norm(states[slots[i], h]) / np.sqrt(got_s.shape[-1])), (i, t, h)
+                    assert np.linalg.norm(err) <= tol * max(np.linalg.norm(out[t][h]), np.linalg.norm(states[slots[i], h]) / np.sqrt(got_s.shape[-1])) + rounding(a, t, h), (i, t, h)
             for h in range(got.shape[1]):
                 assert np.linalg.norm(got_s[slots[i], h] - states[slots[i], h]) <= tol * np.linalg.norm(states[slots[i], h]) , (i, h)
         rows = {t for i, (a, b) in enumerate(self.ranges) if slots[i] >= 0 for t in range(a, b)}
