@@ -83,6 +83,17 @@ __device__ __forceinline__ void split_to_tmem(uint32_t taddr, const float* x, fl
     split16(x, scale, w, w + 8);
     tmem_st16(taddr, w);
 }
+// ... of numbers that are in range as they are
+__device__ __forceinline__ void split_to_tmem(uint32_t taddr, const float* x) {
+    uint32_t w[16];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        w[e] = pack_f16x2(x[2 * e], x[2 * e + 1]);
+        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[e])), l = __fadd2_rn(make_float2(x[2 * e], x[2 * e + 1]), make_float2(-h.x, -h.y));
+        w[8 + e] = pack_f16x2(l.x, l.y);
+    }
+    tmem_st16(taddr, w);
+}
 
 // acc[r] = sum over l < N of rows[r][l] cols[l]: eight rows (pitch AP, read as broadcast vectors) times this lane's column, the
 // even and the odd l in the two halves of packed multiply-adds.  UNROLL steps of four l at a time: all of them at dk <= 64 (5000

@@ -59,23 +59,36 @@ struct Shape {
     static constexpr int KB = D > 64 ? D / 64 : 1;                 // K blocks of 64 elements
     static constexpr int PARTS = WIDE_T ? 2 : 1;                   // fp16 parts of a key, a query, P
     static constexpr int PREPS = WIDE_T && D == 128 ? 1 : 2;       // preparing teams
-    static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = WIDE_T ? 1 : 2;
+    static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = 2;
     static constexpr int PREP_THREADS = 128 * PREPS, CHAIN_THREADS = 256, THREADS = PREP_THREADS + CHAIN_THREADS + 128;
     static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK, T_BYTES = 2 * TILE, P_BYTES = PARTS * TILE;
-    static constexpr int V_BYTES = C * ROWS * (int)sizeof(T);
+    static constexpr bool STAGE_V = !WIDE_T;                       // values through shared memory (fp32: there is no room)
+    static constexpr int V_BYTES = STAGE_V ? C * ROWS * (int)sizeof(T) : 0;
     static constexpr int A_BYTES = (C * AP * 4 + 1023) / 1024 * 1024, X_BYTES = 5 * 1024;
-    // per K stage: g / key scale, g / query scale, beta, g_C; per T stage: weights of D for the state, of D, of P's rows
-    static constexpr int KCO = 3 * C + 4, TCO = 3 * C;
-    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + 10 * ROWS) * 4 + 256;
+    // per K stage: beta g / key scale, g / query scale, beta, g_C; per T stage: weights of D's columns for the state, what undoes P's rows' scales
+    // and T's
+    static constexpr int KCO = 3 * C + 4, TCO = 2 * C + 4;
+    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + 12 * ROWS) * 4 + 256;
     static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
     static_assert(SMEM <= 232448, "shared memory");
     // tensor memory: S operand / D K | Z, X operand, D operand for the outputs (64) ; S Q^T (64) | D (64) | D P^T (64) | per preparing team 64
     static constexpr uint32_t Z_COL = 128, O1_COL = Z_COL + C, D_COL = 256, O2_COL = 320, PREP_COL = 384, TMEM_COLS = 512;
-    // registers: 640 threads start with 96 each; the chain's state rows take what the other roles leave
-    static constexpr bool SPLIT_REGS = THREADS == 640 && D == 128;
-    static constexpr int PREP_REGS = 80, CHAIN_REGS = 128, OUT_REGS = 64;
+    // registers: 640 threads start with 96 each; the roles share them as they need them
+    static constexpr bool SPLIT_REGS = THREADS == 640;
+    static constexpr int PREP_REGS = D == 128 ? 72 : 88, CHAIN_REGS = D == 128 ? 128 : 112, OUT_REGS = 80;
     static_assert(!SPLIT_REGS || 2 * PREP_REGS + 2 * CHAIN_REGS + OUT_REGS <= 5 * 96, "a split beyond the launch's registers waits for ever");
 };
+
+// the largest of m and two magnitudes, in one instruction
+__device__ __forceinline__ float max3(float m, float a, float b) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ float2 pair(float x, float y) { return make_float2(x, y); }
+__device__ __forceinline__ float2 pair(uint32_t x, uint32_t y) { return make_float2(__uint_as_float(x), __uint_as_float(y)); }
+// (the compiler keeps what it knows to be the same in all lanes where the MMAs want it)
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 template <int D, typename T>
 __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(const DeltaArgs a) {
@@ -91,8 +104,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
     float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);
     float* tco_s = kco_s + Z::K_STAGES * Z::KCO;
     float* tok_s = tco_s + Z::T_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
-    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [3][2][ROWS] largest of a half row: S, X, D
-    float* inv_s = max_s + 6 * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
+    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [4][2][ROWS] largest of a half row: S, X, D, D as weighted
+    float* inv_s = max_s + 8 * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
     uint64_t* bars = reinterpret_cast<uint64_t*>(inv_s + 4 * ROWS);
     auto bar_k = [&](int i) { return smem_u32(bars + i % Z::K_STAGES); };           // keys, queries, their weights
     auto bar_kfree = [&](int i) { return smem_u32(bars + 3 + i % Z::K_STAGES); };
@@ -177,7 +190,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         float* X_s = A_s + Z::A_BYTES / 4;                                                      // [32][36]
         float* scale_s = tok_s + team * (128 + 3 * C);
         float *alpha_s = scale_s + 128, *behind_s = alpha_s + C, *total_s = behind_s + C;       // total_s: product of the gates of either warp
-        const uint32_t acc_at = tmem_base + Z::PREP_COL + team * C;
+        const uint32_t acc_at = uniform(tmem_base + Z::PREP_COL + team * C);
         constexpr int VEC = Vec16<T>::N, CPR = D / VEC, LR = CPR < 8 ? CPR : 8;      // 16-byte chunks and lanes per row
         constexpr int PASS_ROWS = 128 / LR, PASSES = 128 / PASS_ROWS, NC = CPR / LR;
         constexpr int BATCH = PASSES * NC > 8 ? 8 / NC : PASSES;                     // passes whose loads are in flight together
@@ -215,24 +228,29 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
                     for (int c = 0; c < NC; ++c) Vec16<T>::unpack(raw[p][c], x + c * VEC);
 #pragma unroll
-                    for (int e = 0; e < NC * VEC; ++e) m = fmaxf(m, fabsf(x[e]));
+                    for (int e = 0; e < NC * VEC; e += 2) m = max3(m, x[e], x[e + 1]);
 #pragma unroll
                     for (int o = LR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                     float sc, inv;
                     pow2_scale(m, NARROW, sc, inv);
-                    if (lr == 0) scale_s[row] = inv;
+#pragma unroll
+                    for (int e = 0; e < NC * VEC; e += 2) {
+                        const float2 y = __fmul2_rn(pair(x[e], x[e + 1]), pair(sc, sc));
+                        x[e] = y.x;
+                        x[e + 1] = y.y;
+                    }
+                    if (lr == 0) scale_s[row] = m > 0x1p-122f ? inv : 0.f;     // (below that the row is nothing in fp16: so is what it undoes)
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
                         const int el = (c * LR + lr) * VEC;
                         uint8_t* dst = KQ_s + (el >> 6) * KQ_BLOCK + row * 128 + ((((el & 63) >> 3) ^ (row & 7)) << 4) + (el & 7) * 2;
                         const float* y = x + c * VEC;
                         if constexpr (VEC == 8) {        // bf16: exact in one fp16 number
-                            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_f16x2(y[0] * sc, y[1] * sc), pack_f16x2(y[2] * sc, y[3] * sc),
-                                                                        pack_f16x2(y[4] * sc, y[5] * sc), pack_f16x2(y[6] * sc, y[7] * sc));
+                            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_f16x2(y[0], y[1]), pack_f16x2(y[2], y[3]), pack_f16x2(y[4], y[5]), pack_f16x2(y[6], y[7]));
                         } else {
                             uint32_t hi[2], lo[2];
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) split2(y[2 * e] * sc, y[2 * e + 1] * sc, hi[e], lo[e]);
+                            for (int e = 0; e < 2; ++e) split2(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
                             *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
                             *reinterpret_cast<uint2*>(dst + KB * KQ_BLOCK) = make_uint2(lo[0], lo[1]);
                         }
@@ -263,10 +281,10 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             if (bar_or(1 + team, 128, fail ? 1 : 0)) { fail = true; break; }
             if (w4 == 0) {          // [K; Q] K^T
                 tc_fence_after();
-                const uint64_t kd = umma_desc(smem_u32(KQ_s));
+                const uint64_t kd = umma_desc(uniform(smem_u32(KQ_s)));
 #pragma unroll 1
                 for (int t = PARTS > 1 ? 2 : 0; t >= 0; --t)                // small terms first: (lo hi, hi lo,) hi hi
-#pragma unroll 1
+#pragma unroll
                     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
@@ -278,7 +296,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             if (pt < C) {
                 if (w4 == 1) g *= total_s[0];
                 else behind *= total_s[1];
-                kco[pt] = g * scale_s[pt];
+                kco[pt] = beta * (g * scale_s[pt]);
                 kco[C + pt] = g * scale_s[C + pt];
                 kco[2 * C + pt] = beta;
                 if (pt == C - 1) kco[3 * C] = g;
@@ -355,46 +373,49 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
                 for (int r = 0; r < 8; ++r) B21[r * AP + col] = -acc[r];
             } else {
+                // P's scale is a bound's, so that one round does: a row's scaled dot products are below 2^15 (128 x 2^4 x 2^4), the keys' scales
+                // are taken relative to the coarsest key's, and gates beyond 1 multiply to `up` at the most
                 const int me = pt - C;
-                const float coef = scale_s[pt];
-                float ratio = 1.f, m = 0.f, sc = 0.f, inv = 0.f;
+                float coarsest = fmaxf(scale_s[lane], scale_s[lane + 32]), up = fmaxf(alpha_s[lane], 1.f) * fmaxf(alpha_s[lane + 32], 1.f);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    coarsest = fmaxf(coarsest, __shfl_xor_sync(0xffffffffu, coarsest, o));
+                    up *= __shfl_xor_sync(0xffffffffu, up, o);
+                }
+                float down, up2, undo, relative;
+                pow2_scale(up, -1, down, up2);                                  // up times down in [1 / 2, 1)
+                pow2_scale(coarsest, 0, relative, undo);                        // (a power of two: relative = 1 / coarsest)
+                const float sc = 0.25f * down;
+                float ratio = 1.f;
                 if (i >= Z::T_STAGES) wait(bar_tfree(i - Z::T_STAGES), t_turn(i - Z::T_STAGES));
-                // once for the row's largest element, once for the operand
+                tco[C + me] = (4.f * up2) * (scale_s[pt] * undo);
 #pragma unroll 1
-                for (int round = 0; round < 2; ++round) {
-                    if (round) {
-                        pow2_scale(m, NARROW, sc, inv);
-                        tco[2 * C + me] = inv;
-                        ratio = 1.f;
+                for (int cb = 3; cb >= 0; --cb) {
+                    uint32_t v[16], hi[8], lo[8];
+                    tmem_ld16(acc_at + cb * 16 + ((uint32_t)(w4 * 32) << 16), v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 12; e >= 0; e -= 4) {
+                        const float4 al = *reinterpret_cast<const float4*>(alpha_s + cb * 16 + e), ki = *reinterpret_cast<const float4*>(scale_s + cb * 16 + e);
+                        const float alv[4] = {al.x, al.y, al.z, al.w}, kiv[4] = {ki.x, ki.y, ki.z, ki.w};
+#pragma unroll
+                        for (int f = 3; f >= 0; --f) {
+                            const int l = cb * 16 + e + f;
+                            const float x = __uint_as_float(v[e + f]) * (kiv[f] * relative);
+                            v[e + f] = __float_as_uint(l <= me ? (ratio * sc) * x : 0.f);
+                            ratio *= l <= me ? alv[f] : 1.f;
+                        }
                     }
-#pragma unroll 1
-                    for (int cb = 3; cb >= 0; --cb) {
-                        uint32_t v[16], hi[8], lo[8];
-                        tmem_ld16(acc_at + cb * 16 + ((uint32_t)(w4 * 32) << 16), v);
-                        tc_wait_ld();
 #pragma unroll
-                        for (int e = 12; e >= 0; e -= 4) {
-                            const float4 al = *reinterpret_cast<const float4*>(alpha_s + cb * 16 + e), ki = *reinterpret_cast<const float4*>(scale_s + cb * 16 + e);
-                            const float alv[4] = {al.x, al.y, al.z, al.w}, kiv[4] = {ki.x, ki.y, ki.z, ki.w};
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (PARTS > 1) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
+                        else hi[e] = pack_f16x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                    }
 #pragma unroll
-                            for (int f = 3; f >= 0; --f) {
-                                const int l = cb * 16 + e + f;
-                                const float x = l <= me ? (coef * ratio) * (__uint_as_float(v[e + f]) * kiv[f]) : 0.f;
-                                ratio *= l <= me ? alv[f] : 1.f;
-                                m = round ? m : fmaxf(m, fabsf(x));
-                                v[e + f] = __float_as_uint(x * sc);
-                            }
-                        }
-                        if (round) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                uint8_t* dst = P_s + me * 128 + (((2 * cb + e) ^ (me & 7)) << 4);
-                                *reinterpret_cast<uint4*>(dst) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-                                if constexpr (PARTS > 1) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
-                            }
-                        }
+                    for (int e = 0; e < 2; ++e) {
+                        uint8_t* dst = P_s + me * 128 + (((2 * cb + e) ^ (me & 7)) << 4);
+                        *reinterpret_cast<uint4*>(dst) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
+                        if constexpr (PARTS > 1) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
                     }
                 }
             }
@@ -421,10 +442,14 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     const float4 x = *reinterpret_cast<const float4*>(A_s + ti * AP + 16 * hf + (q >> 2) * 32 + (q & 3) * 4);
                     t[4 * q] = x.x; t[4 * q + 1] = x.y; t[4 * q + 2] = x.z; t[4 * q + 3] = x.w;
                 }
-                // (what lies above the diagonal is no part of T: the upper right quarter still holds A's zeros)
+                // (what lies above the diagonal is zero, A's there too; one scale for the tile, whose diagonal is 1)
 #pragma unroll
-                for (int q = 0; q < 32; ++q) m = fmaxf(m, fabsf(t[q]));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                for (int q = 0; q < 32; q += 2) m = max3(m, t[q], t[q + 1]);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                if (lane == 0) X_s[w4] = m;
+                bar_or(1 + team, 128, 0);
+                m = fmaxf(fmaxf(X_s[0], X_s[1]), fmaxf(X_s[2], X_s[3]));
                 float sc, inv;
                 pow2_scale(m, NARROW, sc, inv);
 #pragma unroll
@@ -436,10 +461,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     *reinterpret_cast<uint4*>(T_s + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     *reinterpret_cast<uint4*>(T_s + TILE + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
-                if (hf == 0) {
-                    tco[ti] = inv * behind_s[ti];
-                    tco[C + ti] = inv;
-                }
+                if (hf == 0) tco[ti] = behind_s[ti];
+                if (pt == 0) tco[2 * C] = inv;
             }
             proxy_fence();
             arrive(bar_t(i));
@@ -457,14 +480,16 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         const float* other = max_s + (1 - c) * ROWS + r;
         float* state = a.states + seq.slot * a.state_stride + ((long long)hv * a.dv + row_base + r) * D + c * H;
         auto meet = [&] { return bar_or(CHAIN_BARRIER, Z::CHAIN_THREADS, fail ? 1 : 0); };
-        float S[H], m = 0.f;
+        // the row's half, times 2^e; inv_row, scale_row: 2^-e, 2^e.  The exponent changes only when the row's largest element leaves a
+        // window in which two fp16 parts hold it to 22 bits.
+        float S[H], m = 0.f, inv_row = 1.f, scale_row = 1.f;
 #pragma unroll
         for (int e = 0; e < H; e += 4) {
             const float4 x = is_row && !seq.fresh ? __ldcs(reinterpret_cast<const float4*>(state + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
             S[e] = x.x; S[e + 1] = x.y; S[e + 2] = x.z; S[e + 3] = x.w;
         }
 #pragma unroll
-        for (int e = 0; e < H; ++e) m = fmaxf(m, fabsf(S[e]));
+        for (int e = 0; e < H; e += 2) m = max3(m, S[e], S[e + 1]);
         *mine = m;
         meet();
         int issued = 0;                                           // chunks whose last products have been issued
@@ -473,11 +498,24 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             const uint32_t turn = i & 1;
             const float* kco = kco_s + i % Z::K_STAGES * Z::KCO;
             const float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
-            float sc, inv_row;
+            float sc;
             // ---- Z = S K^T, and S Q^T ----
-            pow2_scale(fmaxf(m, *other), WIDE, sc, inv_row);
+            m = fmaxf(m, *other);
+            if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f)) {
+                float inv;
+                pow2_scale(m, WIDE, sc, inv);
 #pragma unroll
-            for (int b = 0; b < HB; ++b) split_to_tmem(s_at + 16 * b, S + 16 * b, sc);
+                for (int e = 0; e < H; e += 2) {
+                    const float2 y = __fmul2_rn(pair(S[e], S[e + 1]), pair(sc, sc));
+                    S[e] = y.x;
+                    S[e + 1] = y.y;
+                }
+                inv_row *= inv;
+                scale_row *= sc;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int b = 0; b < HB; ++b) split_to_tmem(s_at + 16 * b, S + 16 * b);
             if (c == 0) inv_s[turn * ROWS + r] = inv_row;
             tc_wait_st();
             tc_fence_before();
@@ -486,7 +524,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             if (meet()) { fail = true; break; }
             if (issuer) {
                 tc_fence_after();
-                const uint64_t kd = umma_desc(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES));
+                const uint64_t kd = umma_desc(uniform(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES)));
                 bool first = true;
                 auto product = [&](int sp, int kp, int cols) {
 #pragma unroll
@@ -506,38 +544,46 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 }
                 mma_commit(bar_z);
             }
-            wait(bar_v, turn);
+            float val[Z::STAGE_V ? 1 : 32];                       // fp32 values: from global memory, beside the product
+            if constexpr (Z::STAGE_V) {
+                wait(bar_v, turn);
+            } else {
+                const T* vp = static_cast<const T*>(a.v) + seq.begin * a.v_stride + (long long)hv * a.dv + row_base + r;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int t = i * C + 32 * c + e;
+                    val[e] = is_row && t < seq.length ? __ldg(reinterpret_cast<const float*>(vp + t * a.v_stride)) : 0.f;
+                }
+            }
             wait_mma(bar_z, turn);
             tc_fence_after();
             // ---- X = (V^T - Z diag(g)) diag(beta) ----
             float x[32], mx = 0.f;
+            const float2 neg = pair(-inv_row, -inv_row);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 uint32_t v[16];
                 tmem_ld16(z_at + 16 * b, v);
-                float val[16];
+                float u[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    if constexpr (sizeof(T) == 2) val[e] = __bfloat162float(v_s[(32 * c + 16 * b + e) * ROWS + r]);
-                    else val[e] = v_s[(32 * c + 16 * b + e) * ROWS + r];
+                    if constexpr (Z::STAGE_V) u[e] = __bfloat162float(v_s[(32 * c + 16 * b + e) * ROWS + r]);
+                    else u[e] = val[16 * b + e];
                 }
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
                     const float4 gz = *reinterpret_cast<const float4*>(kco + 32 * c + 16 * b + e), be = *reinterpret_cast<const float4*>(kco + 2 * C + 32 * c + 16 * b + e);
-                    const float gzv[4] = {gz.x, gz.y, gz.z, gz.w}, bev[4] = {be.x, be.y, be.z, be.w};
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const float y = bev[f] * fmaf(-gzv[f], __uint_as_float(v[e + f]) * inv_row, val[e + f]);
-                        x[16 * b + e + f] = y;
-                        mx = fmaxf(mx, fabsf(y));
-                    }
+                    const float2 y0 = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), neg), pair(gz.x, gz.y), __fmul2_rn(pair(u[e], u[e + 1]), pair(be.x, be.y)));
+                    const float2 y1 = __ffma2_rn(__fmul2_rn(pair(v[e + 2], v[e + 3]), neg), pair(gz.z, gz.w), __fmul2_rn(pair(u[e + 2], u[e + 3]), pair(be.z, be.w)));
+                    x[16 * b + e] = y0.x; x[16 * b + e + 1] = y0.y; x[16 * b + e + 2] = y1.x; x[16 * b + e + 3] = y1.y;
+                    mx = max3(max3(mx, y0.x, y0.y), y1.x, y1.y);
                 }
             }
             const float g_chunk = kco[3 * C];
             mine[2 * ROWS] = mx;
             if (meet()) { fail = true; break; }
-            if (leader) arrive(bar_vfree);
+            if (Z::STAGE_V && leader) arrive(bar_vfree);
             float inv_x;
             pow2_scale(fmaxf(mx, other[2 * ROWS]), WIDE, sc, inv_x);
 #pragma unroll
@@ -549,7 +595,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             // ---- D = X T^T ----
             if (issuer) {
                 tc_fence_after();
-                const uint64_t td = umma_desc(smem_u32(t_ring + i % Z::T_STAGES * Z::T_BYTES));
+                const uint64_t td = umma_desc(uniform(smem_u32(t_ring + i % Z::T_STAGES * Z::T_BYTES)));
 #pragma unroll
                 for (int t = 2; t >= 0; --t)                      // small terms first: lo hi, hi lo, hi hi
 #pragma unroll
@@ -559,8 +605,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             }
             wait_mma(bar_d, turn);
             tc_fence_after();
-            // ---- D's operands: times g_C / g (and what undoes the keys' scales) for the state, as it is for the outputs, one scale for both ----
-            float md = 0.f;
+            // ---- D's operands: times g_C / g (and what undoes the keys' scales) for the state, as it is for the outputs ----
+            float my = 0.f, me = 0.f;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 uint32_t v[16];
@@ -568,43 +614,41 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e), u = *reinterpret_cast<const float4*>(tco + C + 32 * c + 16 * b + e);
-                    const float wv[4] = {w.x, w.y, w.z, w.w}, uv[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        const float y = __uint_as_float(v[e + f]) * inv_x;
-                        x[16 * b + e + f] = y;
-                        md = fmaxf(md, fmaxf(fabsf(y * wv[f]), fabsf(y * uv[f])));
-                    }
+                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
+                    const float2 d0 = pair(v[e], v[e + 1]), d1 = pair(v[e + 2], v[e + 3]), e0 = __fmul2_rn(d0, pair(w.x, w.y)), e1 = __fmul2_rn(d1, pair(w.z, w.w));
+                    x[16 * b + e] = d0.x; x[16 * b + e + 1] = d0.y; x[16 * b + e + 2] = d1.x; x[16 * b + e + 3] = d1.y;
+                    my = max3(max3(my, d0.x, d0.y), d1.x, d1.y);
+                    me = max3(max3(me, e0.x, e0.y), e1.x, e1.y);
                 }
             }
-            mine[4 * ROWS] = md;
+            mine[4 * ROWS] = my;
+            mine[6 * ROWS] = me;
+            const float undo = inv_x * tco[2 * C];
             if (meet()) { fail = true; break; }
-            float inv_d;
-            pow2_scale(fmaxf(md, other[4 * ROWS]), WIDE, sc, inv_d);
-            if (c == 0) inv_s[(2 + turn) * ROWS + r] = inv_d;
+            float inv_d, inv_e, sc_e;
+            pow2_scale(fmaxf(my, other[4 * ROWS]), WIDE, sc, inv_d);
+            pow2_scale(fmaxf(me, other[6 * ROWS]), WIDE, sc_e, inv_e);
+            if (c == 0) inv_s[(2 + turn) * ROWS + r] = inv_d * undo;
+            const float back = (inv_e * undo) * scale_row;            // of D K, to the state rows' units
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 float y[16];
-                uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    const float4 w4 = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
-                    y[e] = x[16 * b + e] * w4.x; y[e + 1] = x[16 * b + e + 1] * w4.y; y[e + 2] = x[16 * b + e + 2] * w4.z; y[e + 3] = x[16 * b + e + 3] * w4.w;
+                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
+                    const float2 e0 = __fmul2_rn(pair(x[16 * b + e], x[16 * b + e + 1]), pair(w.x, w.y)), e1 = __fmul2_rn(pair(x[16 * b + e + 2], x[16 * b + e + 3]), pair(w.z, w.w));
+                    y[e] = e0.x; y[e + 1] = e0.y; y[e + 2] = e1.x; y[e + 3] = e1.y;
                 }
-                split16(y, sc, w, w + 8);
-                tmem_st16(d_at + 16 * b, w);
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const float4 u4 = *reinterpret_cast<const float4*>(tco + C + 32 * c + 16 * b + e);
-                    y[e] = x[16 * b + e] * u4.x; y[e + 1] = x[16 * b + e + 1] * u4.y; y[e + 2] = x[16 * b + e + 2] * u4.z; y[e + 3] = x[16 * b + e + 3] * u4.w;
-                }
+                split_to_tmem(d_at + 16 * b, y, sc_e);
                 if constexpr (PARTS > 1) {
-                    split16(y, sc, w, w + 8);
-                    tmem_st16(z_at + 16 * b, w);
+                    split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
                 } else {
+                    uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = pack_f16x2(y[2 * e] * sc, y[2 * e + 1] * sc);
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 d = __fmul2_rn(pair(x[16 * b + 2 * e], x[16 * b + 2 * e + 1]), pair(sc, sc));
+                        w[e] = pack_f16x2(d.x, d.y);
+                    }
                     tmem_st8(z_at + 16 * b, w);
                 }
             }
@@ -614,8 +658,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             // ---- D K over the S operand (read by now), and D P^T ----
             if (issuer) {
                 tc_fence_after();
-                const uint64_t kd = umma_desc_mn(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES), KQ_BLOCK);
-                const uint64_t pd = umma_desc(smem_u32(p_ring + i % Z::T_STAGES * Z::P_BYTES));
+                const uint64_t kd = umma_desc_mn(uniform(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES)), KQ_BLOCK);
+                const uint64_t pd = umma_desc(uniform(smem_u32(p_ring + i % Z::T_STAGES * Z::P_BYTES)));
                 bool first = true;
                 auto product = [&](int dp, int kp) {
 #pragma unroll
@@ -649,9 +693,11 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 tmem_ld16(s_at + 16 * b, v);
                 tc_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    S[16 * b + e] = fmaf(g_chunk, S[16 * b + e], __uint_as_float(v[e]) * inv_d);
-                    m = fmaxf(m, fabsf(S[16 * b + e]));
+                for (int e = 0; e < 16; e += 2) {
+                    const float2 y2 = __ffma2_rn(pair(g_chunk, g_chunk), pair(S[16 * b + e], S[16 * b + e + 1]), __fmul2_rn(pair(v[e], v[e + 1]), pair(back, back)));
+                    S[16 * b + e] = y2.x;
+                    S[16 * b + e + 1] = y2.y;
+                    m = max3(m, y2.x, y2.y);
                 }
             }
             *mine = m;
@@ -661,7 +707,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
         if (!fail && is_row) {
 #pragma unroll
-            for (int e = 0; e < H; e += 4) __stcs(reinterpret_cast<float4*>(state + e), make_float4(S[e], S[e + 1], S[e + 2], S[e + 3]));
+            for (int e = 0; e < H; e += 4) __stcs(reinterpret_cast<float4*>(state + e), make_float4(S[e] * inv_row, S[e + 1] * inv_row, S[e + 2] * inv_row, S[e + 3] * inv_row));
         }
     } else {
         // =============================== VALUES IN, OUTPUTS OUT ===============================
@@ -684,42 +730,67 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
             arrive(bar_v);
         };
-        if (n > 0) load_values(0);
+        if (Z::STAGE_V && n > 0) load_values(0);
 #pragma unroll 1
         for (int i = 0; i < n && !fail; ++i) {
             const uint32_t turn = i & 1;
             const float* kco = kco_s + i % Z::K_STAGES * Z::KCO + C;
-            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO + 2 * C;
-            if (i + 1 < n) {
+            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO + C;
+            if (Z::STAGE_V && i + 1 < n) {
                 wait(bar_vfree, turn);
                 if (!fail) load_values(i + 1);
+            }
+            if (!Z::STAGE_V && i + 1 < n) {                           // the lines of the next chunk's values into L2
+                const int t = min((i + 1) * C + (ot >> 1), seq.length - 1);
+                for (int x = (ot & 1) * 32; x < rows; x += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(vp + t * a.v_stride + x));
             }
             wait(bar_o, turn);
             // (the warps of this team do not wait for one another; a warp's threads leave together)
             if (__any_sync(0xffffffffu, fail)) { fail = true; break; }
             tc_fence_after();
             const float inv_row = inv_s[turn * ROWS + r], inv_d = inv_s[(2 + turn) * ROWS + r];
-#pragma unroll 1
-            for (int b = 0; b < 4; ++b) {
+            // read out first and stored behind that, so that the chain may go on (fp32: half of it, for want of registers)
+            constexpr int PER = sizeof(T) == 2 ? 2 : 1, FIRST = PER == 2 ? 0 : 2;      // outputs per register; blocks of 16 stored at once
+            T* dst = op + (long long)(i * C) * a.out_stride;
+            const int left = is_row ? seq.length - i * C : 0;
+            uint32_t o[(4 - FIRST) * 16 / PER];
+            auto block = [&](int b, uint32_t* to) {
                 uint32_t v[16], w[16];
                 tmem_ld16(tmem_base + lanes + Z::O1_COL + 16 * b, v);
                 tmem_ld16(tmem_base + lanes + Z::O2_COL + 16 * b, w);
                 tc_wait_ld();
-                if (b == 3) {
-                    tc_fence_before();
-                    arrive(bar_ofree);
-                }
-                T* dst = op + (long long)(i * C + 16 * b) * a.out_stride;
-                const int left = seq.length - (i * C + 16 * b);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float o = fmaf(__uint_as_float(v[e]) * inv_row, kco[16 * b + e], __uint_as_float(w[e]) * inv_d * tco[16 * b + e]);
-                    if (is_row && e < left) {
-                        if constexpr (sizeof(T) == 2) dst[e * a.out_stride] = __float2bfloat16_rn(o);
-                        else dst[e * a.out_stride] = o;
+                for (int e = 0; e < 16; e += 2) {
+                    const float2 gq = *reinterpret_cast<const float2*>(kco + 16 * b + e), ps = *reinterpret_cast<const float2*>(tco + 16 * b + e);
+                    const float2 y = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), pair(inv_row, inv_row)), gq, __fmul2_rn(__fmul2_rn(pair(w[e], w[e + 1]), pair(inv_d, inv_d)), ps));
+                    if constexpr (PER == 2) {
+                        to[e / 2] = sm100::pack_bf16x2(y.x, y.y);
+                    } else {
+                        to[e] = __float_as_uint(y.x);
+                        to[e + 1] = __float_as_uint(y.y);
                     }
                 }
+            };
+            auto store = [&](int first, int count, const uint32_t* from) {
+#pragma unroll
+                for (int e = 0; e < count; ++e) {
+                    if (first + e < left) {
+                        if constexpr (PER == 2) *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(from[e / 2] >> (16 * (e & 1)));
+                        else *dst = __uint_as_float(from[e]);
+                    }
+                    dst += a.out_stride;
+                }
+            };
+#pragma unroll 1
+            for (int b = 0; b < FIRST; ++b) {
+                block(b, o);
+                store(16 * b, 16, o);
             }
+#pragma unroll
+            for (int b = FIRST; b < 4; ++b) block(b, o + (b - FIRST) * 16 / PER);
+            tc_fence_before();
+            arrive(bar_ofree);
+            store(16 * FIRST, C - 16 * FIRST, o);
             arrive(bar_kfree(i));
             arrive(bar_tfree(i));
         }
