@@ -135,8 +135,7 @@ _NATIVE_CALLS = ("init_state", "init_states", "prefill", "reorder", "select_beam
                  "release")
 
 
-def _native_caller(lib, handle, cfg):
-    """The native marshalling object of one context (see csrc/onela_pycall.cpp)."""
+def _pycall_module():
     global _pycall
     if _pycall is None:
         path = pycall_path()
@@ -146,8 +145,26 @@ def _native_caller(lib, handle, cfg):
         spec = importlib.util.spec_from_file_location("_onela_pycall", path)
         _pycall = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(_pycall)
+    return _pycall
+
+
+_operators = None
+
+
+def _native_operators():
+    """The native marshalling object of the operators without a context."""
+    global _operators
+    if _operators is None:
+        lib = load_library()
+        _operators = _pycall_module().Operators(tuple(ctypes.cast(getattr(lib, n), c_void_p).value
+                                                      for n in ("onela_norm_rotate", "onela_delta_rule", "onela_sample_tokens")))
+    return _operators
+
+
+def _native_caller(lib, handle, cfg):
+    """The native marshalling object of one context (see csrc/onela_pycall.cpp)."""
     fns = tuple(ctypes.cast(getattr(lib, n), c_void_p).value for n in _CALLER_FUNCTIONS)
-    return _pycall.Caller(handle.value, ctypes.addressof(cfg), fns)
+    return _pycall_module().Caller(handle.value, ctypes.addressof(cfg), fns)
 
 
 def _no_native_call(*_):
@@ -245,6 +262,10 @@ def onela_norm_rotate(q, k, q_out, k_out, norm="l2", eps=1e-6, q_scale=1.0, q_we
     """Norms of queries and keys per head with the rotation by position (see onela.h).  q [N, Hq, d], k [N, Hk, d], bf16 or fp32, tokens
     may be strided (slices of one projection); q_out and k_out take the results and may be q and k.  norm: "l2", "rms" (weights [d]
     fp32, optional) or None.  positions int32 [N] and inv_freq fp32 [r / 2] turn the first r elements of each head."""
+    st = (_operators or _native_operators()).norm_rotate(q, k, q_out, k_out, _NORM_CODE.get(norm, -1), eps, q_scale, q_weight, k_weight, positions, inv_freq, interleaved,
+                                                         stream)
+    if st <= 0:
+        return _check(st, "onela_norm_rotate")
     dt, dev = _rec_dtype(q, "q"), q.device
     if q.dim() != 3:
         raise ValueError(f"q: expected [tokens, heads, d], got {tuple(q.shape)}")
@@ -270,6 +291,9 @@ def onela_delta_rule(q, k, v, alpha, beta, states, out, starts=None, slots=None,
     fp32; states [slots, Hv, dv, dk] fp32, updated in place; all may be strided in their first dimension.  starts int32 [n + 1] (None: one token
     per sequence), slots int32 [n] (None: sequence i has state i; negative: padding), fresh int32 [n] (not 0: from the zero state), status int32
     [2] or None.  max_tokens: the longest sequence that is expected."""
+    st = (_operators or _native_operators()).delta_rule(q, k, v, alpha, beta, states, out, starts, slots, fresh, max_tokens, status, stream)
+    if st <= 0:
+        return _check(st, "onela_delta_rule")
     dt, dev, f32, i32 = _rec_dtype(q, "q"), q.device, torch.float32, torch.int32
     if q.dim() != 3 or not isinstance(v, torch.Tensor) or v.dim() != 3:
         raise ValueError("q, v: expected [tokens, heads, d]")
@@ -292,6 +316,9 @@ def onela_delta_rule(q, k, v, alpha, beta, states, out, starts=None, slots=None,
 def onela_sample_tokens(logits, uniforms, tokens_out, temperature=None, top_k=None, top_p=None, min_p=None, logprobs_out=None, stream=None) -> None:
     """One token per row of logits [R, V] (bf16 or fp32, rows may be strided) from uniforms fp32 [R] into tokens_out int32 [R] (see onela.h).
     temperature, top_p, min_p fp32 [R], top_k int32 [R]: None where not wanted; logprobs_out fp32 [R] or None."""
+    st = (_operators or _native_operators()).sample_tokens(logits, uniforms, tokens_out, temperature, top_k, top_p, min_p, logprobs_out, stream)
+    if st <= 0:
+        return _check(st, "onela_sample_tokens")
     dt, dev, f32 = _rec_dtype(logits, "logits"), logits.device, torch.float32
     if logits.dim() != 2:
         raise ValueError(f"logits: expected [rows, vocabulary], got {tuple(logits.shape)}")
