@@ -3,9 +3,10 @@
 // A head vector x of d elements becomes y = x / sqrt(sum x^2 + eps) or x / sqrt(mean x^2 + eps) * w, its first r elements turn in pairs
 // by the angle position * inv_freq[i], queries are scaled.  Every element is read once and written once, so HBM bounds it.
 //
-// A row is one (token, head), queries' and keys' heads of a token behind one another; 4 to 32 lanes share it, 8 elements (16 bytes of
-// bf16, 32 of fp32) each, and a thread has ROWS rows in flight.  The angles belong to the token: a CTA, whose rows are consecutive, forms
-// cosine and sine of its few tokens once in shared memory.  position * inv_freq is exact in 64 bits (31 + 24 bits; two more than fit are
+// A row is one (token, head); 4 to 32 lanes share it, 8 elements (16 bytes of bf16, 32 of fp32) each, and a thread has ROWS rows in flight.
+// A CTA takes a few whole tokens, queries' and keys' heads alike: as many as fill its passes of rows best (18 heads of 256 in passes of 32
+// rows: 16 tokens are 9 full passes, one token would leave 14 of 32 rows idle), one where the call is too small to spread.  The angles belong to the token:
+// cosine and sine are formed once per CTA, in shared memory.  position * inv_freq is exact in 64 bits (31 + 24 bits; two more than fit are
 // rounded), reduced there to a fraction of a turn, and only the fraction goes through the fp32 functions, so far positions lose nothing.
 // Elements i and i + r / 2 lie in different lanes of a row (r is a multiple of 16), 8 shuffles away.
 #include <algorithm>
@@ -16,7 +17,7 @@
 namespace onela {
 namespace {
 
-constexpr int THREADS = 256, ROWS = 4;
+constexpr int THREADS = 256, ROWS = 4, OCCUPANCY = 5;
 
 struct NormArgs {
     const void *q, *k;
@@ -26,127 +27,152 @@ struct NormArgs {
     const float* inv_freq;
     long long q_stride, k_stride, q_out_stride, k_out_stride, n_tokens;
     int32_t hq, heads, dim, rotary, interleaved, norm;
-    float eps, q_scale;
+    float eps, q_scale, inv_dim;
+    int32_t tokens;                                         // of a CTA
+    uint32_t magic;                                         // of a division by `heads`
 };
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x) {
-    Vec16<float>::load(p, x);
-    Vec16<float>::load(p + 4, x + 4);
-}
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float* x) { Vec16<__nv_bfloat16>::load(p, x); }
+struct Raw {                                            // 8 elements as they lie in memory
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int c = 0; c < (int)sizeof(T) / 2; ++c) w[c] = __ldg(reinterpret_cast<const uint4*>(p) + c);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int c = 0; c < (int)sizeof(T) / 2; ++c) w[c] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void unpack(float2* x) const {
+        float y[8];
+#pragma unroll
+        for (int c = 0; c < (int)sizeof(T) / 2; ++c) Vec16<T>::unpack(w[c], y + c * Vec16<T>::N);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = make_float2(y[2 * e], y[2 * e + 1]);
+    }
+};
+enum { NO_ROTATION, HALVES, INTERLEAVED };
 
-template <typename T, int LPR>
-__global__ void __launch_bounds__(THREADS) norm_rotate_kernel(const NormArgs a) {
+template <typename T, int LPR, int ROTATION>
+__global__ void __launch_bounds__(THREADS, OCCUPANCY) norm_rotate_kernel(const NormArgs a) {
     constexpr int GROUPS = THREADS / LPR, TILE = GROUPS * ROWS;
     extern __shared__ float turn_s[];                       // [tokens of the CTA][cos r / 2 | sin r / 2]
-    const int half = a.rotary / 2;
-    const long long first = (long long)blockIdx.x * TILE, token0 = first / a.heads;
-    const int head0 = (int)(first - token0 * a.heads);
-    const long long left = a.n_tokens - token0;             // tokens from the CTA's first one on
+    __shared__ __align__(16) float weight_s[2][256];
+    const int half = a.rotary / 2, lane = threadIdx.x % LPR, group = threadIdx.x / LPR, at = lane * 8;
+    const long long token0 = (long long)blockIdx.x * a.tokens;
+    const int tokens = (int)min((long long)a.tokens, a.n_tokens - token0), rows = tokens * a.heads;
+    const bool inside = at < a.dim;
+    const T *q = static_cast<const T*>(a.q) + token0 * a.q_stride + at, *k = static_cast<const T*>(a.k) + token0 * a.k_stride + at;
+    T *q_out = static_cast<T*>(a.q_out) + token0 * a.q_out_stride + at, *k_out = static_cast<T*>(a.k_out) + token0 * a.k_out_stride + at;
+    const bool weights = a.q_weight || a.k_weight;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR, at = lane * 8;
-    const bool inside = at < a.dim;
-    float x[ROWS][8];
-    int tok[ROWS], head[ROWS];
+    auto token_of = [&](int row) { return a.tokens == 1 ? 0 : a.magic ? (int)__umulhi((uint32_t)row, a.magic) : row; };
+    for (int base = 0; base < rows; base += TILE) {
+        Raw<T> raw[ROWS];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int row = head0 + i * GROUPS + group;
-        tok[i] = row / a.heads;
-        head[i] = row - tok[i] * a.heads;
-        if (tok[i] >= left) tok[i] = -1;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-        if (tok[i] >= 0 && inside) {
-            const bool is_q = head[i] < a.hq;
-            const T* p = is_q ? static_cast<const T*>(a.q) + (token0 + tok[i]) * a.q_stride + (long long)head[i] * a.dim
-                              : static_cast<const T*>(a.k) + (token0 + tok[i]) * a.k_stride + (long long)(head[i] - a.hq) * a.dim;
-            load8(p + at, x[i]);
+        for (int i = 0; i < ROWS; ++i) {
+            const int row = base + i * GROUPS + group, tok = token_of(row), head = row - tok * a.heads;
+            if (row < rows && inside) raw[i].load(head < a.hq ? q + tok * a.q_stride + head * a.dim : k + tok * a.k_stride + (head - a.hq) * a.dim);
+            else raw[i].clear();
         }
-    }
-    if (half > 0) {
-        const int span = (int)min(left, (long long)((head0 + TILE - 1) / a.heads + 1));
-        for (int j = threadIdx.x; j < span * half; j += THREADS) {
-            const int t = j / half, f = j - t * half;
-            const double turns = (double)a.positions[token0 + t] * (double)a.inv_freq[f] * 0.15915494309189533577;
-            float s, c;
-            sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-            turn_s[2 * t * half + f] = c;
-            turn_s[(2 * t + 1) * half + f] = s;
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const bool is_q = head[i] < a.hq;
-        if (a.norm != ONELA_NORM_NONE) {
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-#pragma unroll
-            for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float n = 1.f / sqrtf(a.norm == ONELA_NORM_L2 ? sum + a.eps : sum / (float)a.dim + a.eps);
-            const float* w = is_q ? a.q_weight : a.k_weight;
-            if (w && inside) {
-                float wx[8];
-                load8(w + at, wx);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] *= n * wx[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] *= n;
+        if (weights && base == 0) {                         // with the queries' scale in theirs (a rotation passes it on)
+            for (int e = threadIdx.x; e < a.dim; e += THREADS) {
+                weight_s[0][e] = a.q_scale * (a.q_weight ? __ldg(a.q_weight + e) : 1.f);
+                weight_s[1][e] = a.k_weight ? __ldg(a.k_weight + e) : 1.f;
             }
+            if (ROTATION == NO_ROTATION) __syncthreads();
         }
-        if (half > 0) {
-            const float *cs = turn_s + 2 * max(tok[i], 0) * half, *sn = cs + half;
-            if (a.interleaved) {
-                if (at < a.rotary) {
+        if (ROTATION != NO_ROTATION && base == 0) {
+            for (int j = threadIdx.x; j < tokens * half; j += THREADS) {
+                const int t = j / half, f = j - t * half;
+                const double turns = (double)__ldg(a.positions + token0 + t) * (double)__ldg(a.inv_freq + f) * 0.15915494309189533577;
+                float s, c;
+                sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+                turn_s[2 * t * half + f] = c;
+                turn_s[(2 * t + 1) * half + f] = s;
+            }
+            __syncthreads();
+        }
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float c = cs[(at + e) >> 1], s = sn[(at + e) >> 1], u = x[i][e], v = x[i][e + 1];
-                        x[i][e] = u * c - v * s;
-                        x[i][e + 1] = v * c + u * s;
+        for (int i = 0; i < ROWS; ++i) {
+            const int row = base + i * GROUPS + group, tok = token_of(row), head = row - tok * a.heads;
+            const bool is_q = head < a.hq;
+            float2 x[4];
+            raw[i].unpack(x);
+            float scale = 1.f;
+            if (a.norm != ONELA_NORM_NONE) {
+                float2 sums = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums = __ffma2_rn(x[e], x[e], sums);
+                float sum = sums.x + sums.y;
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                scale = rsqrtf(a.norm == ONELA_NORM_L2 ? sum + a.eps : fmaf(sum, a.inv_dim, a.eps));
+            }
+            if (is_q && !weights) scale *= a.q_scale;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __fmul2_rn(x[e], make_float2(scale, scale));
+            if (weights && inside) {
+                const float* w = weight_s[is_q ? 0 : 1] + at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = __fmul2_rn(x[e], *reinterpret_cast<const float2*>(w + 2 * e));
+            }
+            if (ROTATION != NO_ROTATION) {
+                const float *cs = turn_s + 2 * (tok < tokens ? tok : 0) * half, *sn = cs + half;
+                if (ROTATION == INTERLEAVED) {
+                    if (at < a.rotary) {
+                        const float4 c = *reinterpret_cast<const float4*>(cs + at / 2), s = *reinterpret_cast<const float4*>(sn + at / 2);
+                        const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = make_float2(x[e].x * cv[e] - x[e].y * sv[e], x[e].y * cv[e] + x[e].x * sv[e]);
+                    }
+                } else {
+                    const bool low = at < half, turned = at < a.rotary;
+                    const int other = !turned ? lane : low ? lane + half / 8 : lane - half / 8;
+                    float2 y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[e].x = __shfl_sync(0xffffffffu, x[e].x, other, LPR);
+                        y[e].y = __shfl_sync(0xffffffffu, x[e].y, other, LPR);
+                    }
+                    if (turned) {
+                        const int f = low ? at : at - half;
+                        const float2 sign = low ? make_float2(-1.f, -1.f) : make_float2(1.f, 1.f);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = __ffma2_rn(x[e], *reinterpret_cast<const float2*>(cs + f + 2 * e), __fmul2_rn(__fmul2_rn(y[e], sign), *reinterpret_cast<const float2*>(sn + f + 2 * e)));
                     }
                 }
-            } else {
-                const bool low = at < half, turned = at < a.rotary;
-                const int other = low ? lane + half / 8 : lane - half / 8;
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __shfl_sync(0xffffffffu, x[i][e], turned ? other : lane, LPR);
-                if (turned) {
-                    const int f = low ? at : at - half;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float c = cs[f + e], s = low ? -sn[f + e] : sn[f + e];
-                        x[i][e] = x[i][e] * c + y[e] * s;
-                    }
-                }
             }
-        }
-        if (tok[i] >= 0 && inside) {
-            if (is_q) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] *= a.q_scale;
+            if (row < rows && inside) {
+                const float y[8] = {x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
+                store_out<T, 8>(is_q ? q_out + tok * a.q_out_stride + head * a.dim : k_out + tok * a.k_out_stride + (head - a.hq) * a.dim, y);
             }
-            T* p = is_q ? static_cast<T*>(a.q_out) + (token0 + tok[i]) * a.q_out_stride + (long long)head[i] * a.dim
-                        : static_cast<T*>(a.k_out) + (token0 + tok[i]) * a.k_out_stride + (long long)(head[i] - a.hq) * a.dim;
-            store_out<T, 8>(p + at, x[i]);
         }
     }
 }
 
 template <typename T, int LPR>
-cudaError_t launch_lpr(const NormArgs& a, cudaStream_t stream) {
-    constexpr int TILE = THREADS / LPR * ROWS;
-    const long long rows = a.n_tokens * a.heads, ctas = (rows + TILE - 1) / TILE;
-    const size_t smem = (size_t)a.rotary * sizeof(float) * std::min<long long>(a.n_tokens, (a.heads - 1 + TILE - 1) / a.heads + 1);
-    static_assert(THREADS / 4 * ROWS * 32 * 4 <= 48 * 1024, "one head of the narrowest row: cosines and sines of a CTA");
-    return launch_dependent(norm_rotate_kernel<T, LPR>, dim3((unsigned)ctas), dim3(THREADS), smem, stream, a);
+cudaError_t launch_lpr(NormArgs a, cudaStream_t stream) {
+    constexpr int TILE = THREADS / LPR * ROWS, MOST = 16, MIN_CTAS = 4 * 148;
+    a.tokens = 1;
+    double best = 0.0;
+    for (int t = 1; t <= MOST && (t == 1 || (a.n_tokens + t - 1) / t >= MIN_CTAS); ++t) {
+        const long long rows = (long long)t * a.heads;
+        const double full = (double)rows / (double)((rows + TILE - 1) / TILE * TILE);
+        if (full > best + 1e-9) {
+            best = full;
+            a.tokens = t;
+        }
+    }
+    a.magic = (uint32_t)(((1ull << 32) + a.heads - 1) / a.heads);      // (0: one head) exact for rows < 2^16 of up to 2^16 heads; beyond that a CTA has one token
+    if ((long long)a.tokens * a.heads + TILE > 65535) a.tokens = 1;
+    const dim3 grid((unsigned)((a.n_tokens + a.tokens - 1) / a.tokens));
+    const size_t smem = (size_t)a.tokens * a.rotary * sizeof(float);
+    return a.rotary == 0     ? launch_dependent(norm_rotate_kernel<T, LPR, NO_ROTATION>, grid, dim3(THREADS), smem, stream, a)
+           : !a.interleaved ? launch_dependent(norm_rotate_kernel<T, LPR, HALVES>, grid, dim3(THREADS), smem, stream, a)
+                            : launch_dependent(norm_rotate_kernel<T, LPR, INTERLEAVED>, grid, dim3(THREADS), smem, stream, a);
 }
 template <typename T>
 cudaError_t launch_t(const NormArgs& a, cudaStream_t stream) {
@@ -193,7 +219,7 @@ extern "C" onela_status onela_norm_rotate(const onela_norm_rotate_args* g, void*
     if (!(g->eps >= 0.f)) return ONELA_E_INVAL;
     if (g->n_tokens == 0 || g->num_q_heads + g->num_k_heads == 0) return ONELA_OK;
     const long long heads = (long long)g->num_q_heads + g->num_k_heads;
-    if (g->n_tokens > (1ll << 40) / heads || g->n_tokens * heads / (THREADS / 32 * ROWS) >= 0x7fffffffll) return ONELA_E_CAPACITY;    // CTAs of one launch
+    if (g->n_tokens > 0x7fffffffll || heads * g->head_dim > 0x3fffffffll) return ONELA_E_CAPACITY;      // CTAs of one launch, 32-bit offsets within a token
     if (g->rotary_dim > 0 && (!g->positions_dev || !g->inv_freq_dev)) return ONELA_E_INVAL;
     if (!aligned16(g->q_weight_dev) || !aligned16(g->k_weight_dev)) return ONELA_E_INVAL;
     const Rows set[4] = {{static_cast<const char*>(g->q_dev), g->q_stride * es, (long long)g->num_q_heads * g->head_dim * es, g->n_tokens},
@@ -210,7 +236,7 @@ extern "C" onela_status onela_norm_rotate(const onela_norm_rotate_args* g, void*
             if (share_bytes(set[i], set[o])) return ONELA_E_INVAL;
         }
     NormArgs a{g->q_dev, g->k_dev, g->q_out_dev, g->k_out_dev, nullptr, nullptr, g->positions_dev, g->inv_freq_dev, g->q_stride, g->k_stride, g->q_out_stride, g->k_out_stride,
-               g->n_tokens, g->num_q_heads, g->num_q_heads + g->num_k_heads, g->head_dim, g->rotary_dim, g->interleaved != 0, g->norm, g->eps, g->q_scale};
+               g->n_tokens, g->num_q_heads, g->num_q_heads + g->num_k_heads, g->head_dim, g->rotary_dim, g->interleaved != 0, g->norm, g->eps, g->q_scale, 1.f / (float)g->head_dim, 1, 0};
     if (g->norm == ONELA_NORM_RMS) {
         a.q_weight = g->q_weight_dev;
         a.k_weight = g->k_weight_dev;

@@ -65,6 +65,12 @@ def test_head_counts(hq, hk, n):
     _run(n, hq, hk, 128, "bf16", "l2", 32)
 
 
+@pytest.mark.parametrize("hq,hk,d", [(1, 0, 64), (2, 1, 256), (3, 4, 128), (5, 6, 32)])
+def test_many_tokens_per_block(hq, hk, d):
+    """Calls large enough for several tokens in a block; the last block is not full."""
+    _run(12289 + hq, hq, hk, d, "bf16", "rms")
+
+
 def test_far_and_negative_positions():
     pos = torch.tensor([0, 1, -1, 2 ** 31 - 1, -2 ** 31, 10 ** 9, 131071, -7], dtype=torch.int32, device="cuda")
     _run(8, 2, 2, 128, "fp32", None, 128, False, pos)
