@@ -10,6 +10,7 @@
 // rounded), reduced there to a fraction of a turn, and only the fraction goes through the fp32 functions, so far positions lose nothing.
 // Elements i and i + r / 2 lie in different lanes of a row (r is a multiple of 16), 8 shuffles away.
 #include <algorithm>
+#include <cmath>
 
 #include "onela_internal.h"
 #include "onela_layout.cuh"
@@ -17,7 +18,7 @@
 namespace onela {
 namespace {
 
-constexpr int THREADS = 256, ROWS = 4, OCCUPANCY = 5;
+constexpr int THREADS = 256, ROWS_IN_FLIGHT = 4, OCCUPANCY = 4;
 
 struct NormArgs {
     const void *q, *k;
@@ -27,7 +28,7 @@ struct NormArgs {
     const float* inv_freq;
     long long q_stride, k_stride, q_out_stride, k_out_stride, n_tokens;
     int32_t hq, heads, dim, rotary, interleaved, norm;
-    float eps, q_scale, inv_dim;
+    float eps, q_scale, sum_weight;                         // sum_weight: of the sum of squares beside eps
     int32_t tokens;                                         // of a CTA
     uint32_t magic;                                         // of a division by `heads`
 };
@@ -53,133 +54,180 @@ struct Raw {                                            // 8 elements as they li
 };
 enum { NO_ROTATION, HALVES, INTERLEAVED };
 
-template <typename T, int LPR, int ROTATION>
+// LPR lanes per row, CHUNKS pieces of 8 elements per lane (piece c of lane l: elements 8 (c LPR + l) ..)
+template <typename T, int LPR, int CHUNKS, int ROTATION>
 __global__ void __launch_bounds__(THREADS, OCCUPANCY) norm_rotate_kernel(const NormArgs a) {
-    constexpr int GROUPS = THREADS / LPR, TILE = GROUPS * ROWS;
-    extern __shared__ float turn_s[];                       // [tokens of the CTA][cos r / 2 | sin r / 2]
+    constexpr int GROUPS = THREADS / LPR, ROWS = ROWS_IN_FLIGHT / CHUNKS, TILE = GROUPS * ROWS;
+    extern __shared__ __align__(16) float turn_s[];         // [tokens of the CTA][cos r / 2 | sin r / 2 | -sin r / 2]
     __shared__ __align__(16) float weight_s[2][256];
     const int half = a.rotary / 2, lane = threadIdx.x % LPR, group = threadIdx.x / LPR, at = lane * 8;
     const long long token0 = (long long)blockIdx.x * a.tokens;
     const int tokens = (int)min((long long)a.tokens, a.n_tokens - token0), rows = tokens * a.heads;
-    const bool inside = at < a.dim;
     const T *q = static_cast<const T*>(a.q) + token0 * a.q_stride + at, *k = static_cast<const T*>(a.k) + token0 * a.k_stride + at;
     T *q_out = static_cast<T*>(a.q_out) + token0 * a.q_out_stride + at, *k_out = static_cast<T*>(a.k_out) + token0 * a.k_out_stride + at;
     const bool weights = a.q_weight || a.k_weight;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    auto token_of = [&](int row) { return a.tokens == 1 ? 0 : a.magic ? (int)__umulhi((uint32_t)row, a.magic) : row; };
+    // (a CTA's tokens lie within 2^31 elements: launch_shape)
+    const int q_step = (int)a.q_stride, k_step = (int)a.k_stride, q_out_step = (int)a.q_out_stride, k_out_step = (int)a.k_out_stride;
+    auto token_of = [&](int row) { return (int)__umulhi((uint32_t)row, a.magic); };
     for (int base = 0; base < rows; base += TILE) {
-        Raw<T> raw[ROWS];
+        Raw<T> raw[ROWS][CHUNKS];
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             const int row = base + i * GROUPS + group, tok = token_of(row), head = row - tok * a.heads;
-            if (row < rows && inside) raw[i].load(head < a.hq ? q + tok * a.q_stride + head * a.dim : k + tok * a.k_stride + (head - a.hq) * a.dim);
-            else raw[i].clear();
-        }
-        if (weights && base == 0) {                         // with the queries' scale in theirs (a rotation passes it on)
-            for (int e = threadIdx.x; e < a.dim; e += THREADS) {
-                weight_s[0][e] = a.q_scale * (a.q_weight ? __ldg(a.q_weight + e) : 1.f);
-                weight_s[1][e] = a.k_weight ? __ldg(a.k_weight + e) : 1.f;
+            const bool is_q = head < a.hq;
+            const T* p = (is_q ? q : k) + (tok * (is_q ? q_step : k_step) + (is_q ? head : head - a.hq) * a.dim);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (row < rows && at + c * (LPR * 8) < a.dim) raw[i][c].load(p + c * (LPR * 8));
+                else raw[i][c].clear();
             }
-            if (ROTATION == NO_ROTATION) __syncthreads();
         }
-        if (ROTATION != NO_ROTATION && base == 0) {
-            for (int j = threadIdx.x; j < tokens * half; j += THREADS) {
-                const int t = j / half, f = j - t * half;
-                const double turns = (double)__ldg(a.positions + token0 + t) * (double)__ldg(a.inv_freq + f) * 0.15915494309189533577;
-                float s, c;
-                sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-                turn_s[2 * t * half + f] = c;
-                turn_s[(2 * t + 1) * half + f] = s;
+        if (base == 0) {
+            if (weights) {                                  // with the queries' scale in theirs (a rotation passes it on)
+                for (int e = threadIdx.x; e < a.dim; e += THREADS) {
+                    weight_s[0][e] = a.q_scale * (a.q_weight ? __ldg(a.q_weight + e) : 1.f);
+                    weight_s[1][e] = a.k_weight ? __ldg(a.k_weight + e) : 1.f;
+                }
             }
-            __syncthreads();
+            if (ROTATION != NO_ROTATION) {
+                for (int j = threadIdx.x; j < tokens * half; j += THREADS) {
+                    const int t = j / half, f = j - t * half;
+                    const double turns = (double)__ldg(a.positions + token0 + t) * (double)__ldg(a.inv_freq + f) * 0.15915494309189533577;
+                    float s, c;
+                    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+                    float* to = turn_s + 3 * t * half + f;
+                    to[0] = c;
+                    to[half] = s;
+                    to[2 * half] = -s;
+                }
+            }
+            if (weights || ROTATION != NO_ROTATION) __syncthreads();
         }
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             const int row = base + i * GROUPS + group, tok = token_of(row), head = row - tok * a.heads;
             const bool is_q = head < a.hq;
-            float2 x[4];
-            raw[i].unpack(x);
-            float scale = 1.f;
+            float2 x[CHUNKS][4];
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) raw[i][c].unpack(x[c]);
+            float scale = is_q && !weights ? a.q_scale : 1.f;
             if (a.norm != ONELA_NORM_NONE) {
                 float2 sums = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sums = __ffma2_rn(x[e], x[e], sums);
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sums = __ffma2_rn(x[c][e], x[c][e], sums);
                 float sum = sums.x + sums.y;
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                scale = rsqrtf(a.norm == ONELA_NORM_L2 ? sum + a.eps : fmaf(sum, a.inv_dim, a.eps));
+                scale *= rsqrtf(fmaf(sum, a.sum_weight, a.eps));
             }
-            if (is_q && !weights) scale *= a.q_scale;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __fmul2_rn(x[e], make_float2(scale, scale));
-            if (weights && inside) {
+            if (weights) {
                 const float* w = weight_s[is_q ? 0 : 1] + at;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = __fmul2_rn(x[e], *reinterpret_cast<const float2*>(w + 2 * e));
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {        // (what lies behind the row's end is not stored)
+                        const float4 w4 = *reinterpret_cast<const float4*>(w + c * (LPR * 8) + 2 * e);
+                        x[c][e] = __fmul2_rn(x[c][e], __fmul2_rn(make_float2(w4.x, w4.y), make_float2(scale, scale)));
+                        x[c][e + 1] = __fmul2_rn(x[c][e + 1], __fmul2_rn(make_float2(w4.z, w4.w), make_float2(scale, scale)));
+                    }
+            } else {
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[c][e] = __fmul2_rn(x[c][e], make_float2(scale, scale));
             }
             if (ROTATION != NO_ROTATION) {
-                const float *cs = turn_s + 2 * (tok < tokens ? tok : 0) * half, *sn = cs + half;
+                const float* cs = turn_s + 3 * (tok < tokens ? tok : 0) * half;
                 if (ROTATION == INTERLEAVED) {
-                    if (at < a.rotary) {
-                        const float4 c = *reinterpret_cast<const float4*>(cs + at / 2), s = *reinterpret_cast<const float4*>(sn + at / 2);
-                        const float cv[4] = {c.x, c.y, c.z, c.w}, sv[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = make_float2(x[e].x * cv[e] - x[e].y * sv[e], x[e].y * cv[e] + x[e].x * sv[e]);
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        const int el = at + c * (LPR * 8);
+                        if (el < a.rotary) {
+                            const float4 co = *reinterpret_cast<const float4*>(cs + el / 2), si = *reinterpret_cast<const float4*>(cs + half + el / 2);
+                            const float cv[4] = {co.x, co.y, co.z, co.w}, sv[4] = {si.x, si.y, si.z, si.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[c][e] = make_float2(x[c][e].x * cv[e] - x[c][e].y * sv[e], x[c][e].y * cv[e] + x[c][e].x * sv[e]);
+                        }
                     }
                 } else {
-                    const bool low = at < half, turned = at < a.rotary;
-                    const int other = !turned ? lane : low ? lane + half / 8 : lane - half / 8;
-                    float2 y[4];
+                    // x (of the lower or upper half) with its partner y
+                    auto turn = [&](float2* v, const float2* y, int f, bool low) {
+                        const float *cp = cs + f, *sp = cp + (low ? 2 * half : half);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[e].x = __shfl_sync(0xffffffffu, x[e].x, other, LPR);
-                        y[e].y = __shfl_sync(0xffffffffu, x[e].y, other, LPR);
-                    }
-                    if (turned) {
-                        const int f = low ? at : at - half;
-                        const float2 sign = low ? make_float2(-1.f, -1.f) : make_float2(1.f, 1.f);
+                        for (int e = 0; e < 4; e += 2) {
+                            const float4 co = *reinterpret_cast<const float4*>(cp + 2 * e), si = *reinterpret_cast<const float4*>(sp + 2 * e);
+                            v[e] = __ffma2_rn(v[e], make_float2(co.x, co.y), __fmul2_rn(y[e], make_float2(si.x, si.y)));
+                            v[e + 1] = __ffma2_rn(v[e + 1], make_float2(co.z, co.w), __fmul2_rn(y[e + 1], make_float2(si.z, si.w)));
+                        }
+                    };
+                    if (CHUNKS == 2 && half == LPR * 8) {   // the halves are a lane's two pieces
+                        float2 lower[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = __ffma2_rn(x[e], *reinterpret_cast<const float2*>(cs + f + 2 * e), __fmul2_rn(__fmul2_rn(y[e], sign), *reinterpret_cast<const float2*>(sn + f + 2 * e)));
+                        for (int e = 0; e < 4; ++e) lower[e] = x[0][e];
+                        turn(x[0], x[CHUNKS - 1], at, true);
+                        turn(x[CHUNKS - 1], lower, at, false);
+                    } else {                                // both halves lie in the lanes' first pieces
+                        const bool low = at < half, turned = at < a.rotary;
+                        const int other = !turned ? lane : low ? lane + half / 8 : lane - half / 8;
+                        float2 y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[e].x = __shfl_sync(0xffffffffu, x[0][e].x, other, LPR);
+                            y[e].y = __shfl_sync(0xffffffffu, x[0][e].y, other, LPR);
+                        }
+                        if (turned) turn(x[0], y, low ? at : at - half, low);
                     }
                 }
             }
-            if (row < rows && inside) {
-                const float y[8] = {x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
-                store_out<T, 8>(is_q ? q_out + tok * a.q_out_stride + head * a.dim : k_out + tok * a.k_out_stride + (head - a.hq) * a.dim, y);
+            T* p = (is_q ? q_out : k_out) + (tok * (is_q ? q_out_step : k_out_step) + (is_q ? head : head - a.hq) * a.dim);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (row < rows && at + c * (LPR * 8) < a.dim) {
+                    const float y[8] = {x[c][0].x, x[c][0].y, x[c][1].x, x[c][1].y, x[c][2].x, x[c][2].y, x[c][3].x, x[c][3].y};
+                    store_out<T, 8>(p + c * (LPR * 8), y);
+                }
             }
         }
     }
 }
 
-template <typename T, int LPR>
-cudaError_t launch_lpr(NormArgs a, cudaStream_t stream) {
-    constexpr int TILE = THREADS / LPR * ROWS, MOST = 16, MIN_CTAS = 4 * 148;
+template <typename T, int LPR, int CHUNKS>
+cudaError_t launch_shape(NormArgs a, cudaStream_t stream) {
+    // tokens per CTA: the fewest passes of rows in a row on one place of an SM (whole waves of CTAs while there are few)
+    constexpr int TILE = THREADS / LPR * (ROWS_IN_FLIGHT / CHUNKS), MOST = 16, PLACES = 148 * OCCUPANCY;
     a.tokens = 1;
-    double best = 0.0;
-    for (int t = 1; t <= MOST && (t == 1 || (a.n_tokens + t - 1) / t >= MIN_CTAS); ++t) {
-        const long long rows = (long long)t * a.heads;
-        const double full = (double)rows / (double)((rows + TILE - 1) / TILE * TILE);
-        if (full > best + 1e-9) {
-            best = full;
+    double best = 1e30;
+    for (int t = 1; t <= MOST; ++t) {
+        // (a token's number within the CTA is a product: rows below 2^16; offsets within the CTA have 32 bits)
+        if (t > 1 && ((long long)t * a.heads + TILE > 65535 || a.heads == 1 || std::max(std::max(a.q_stride, a.k_stride), std::max(a.q_out_stride, a.k_out_stride)) > (1ll << 26))) break;
+        const long long passes = ((long long)t * a.heads + TILE - 1) / TILE;
+        const double waves = (double)((a.n_tokens + t - 1) / t) / PLACES, cost = (double)passes * (waves < 4 ? std::ceil(waves) : waves);
+        if (cost < best * (1 - 1e-9)) {
+            best = cost;
             a.tokens = t;
         }
     }
-    a.magic = (uint32_t)(((1ull << 32) + a.heads - 1) / a.heads);      // (0: one head) exact for rows < 2^16 of up to 2^16 heads; beyond that a CTA has one token
-    if ((long long)a.tokens * a.heads + TILE > 65535) a.tokens = 1;
+    a.magic = a.tokens > 1 ? (uint32_t)(((1ull << 32) + a.heads - 1) / a.heads) : 0;      // row * magic / 2^32 = row / heads; one token: 0
     const dim3 grid((unsigned)((a.n_tokens + a.tokens - 1) / a.tokens));
-    const size_t smem = (size_t)a.tokens * a.rotary * sizeof(float);
-    return a.rotary == 0     ? launch_dependent(norm_rotate_kernel<T, LPR, NO_ROTATION>, grid, dim3(THREADS), smem, stream, a)
-           : !a.interleaved ? launch_dependent(norm_rotate_kernel<T, LPR, HALVES>, grid, dim3(THREADS), smem, stream, a)
-                            : launch_dependent(norm_rotate_kernel<T, LPR, INTERLEAVED>, grid, dim3(THREADS), smem, stream, a);
+    const size_t smem = (size_t)a.tokens * a.rotary / 2 * 3 * sizeof(float);
+    return a.rotary == 0     ? launch_dependent(norm_rotate_kernel<T, LPR, CHUNKS, NO_ROTATION>, grid, dim3(THREADS), smem, stream, a)
+           : !a.interleaved ? launch_dependent(norm_rotate_kernel<T, LPR, CHUNKS, HALVES>, grid, dim3(THREADS), smem, stream, a)
+                            : launch_dependent(norm_rotate_kernel<T, LPR, CHUNKS, INTERLEAVED>, grid, dim3(THREADS), smem, stream, a);
 }
+// Two pieces per lane where a rotation's partners then share a lane or lie in the first pieces: half the lanes' work per row that
+// does not depend on its width.
 template <typename T>
 cudaError_t launch_t(const NormArgs& a, cudaStream_t stream) {
-    if (a.dim <= 32) return launch_lpr<T, 4>(a, stream);
-    if (a.dim <= 64) return launch_lpr<T, 8>(a, stream);
-    if (a.dim <= 128) return launch_lpr<T, 16>(a, stream);
-    return launch_lpr<T, 32>(a, stream);
+    const int lpr = a.dim <= 64 ? 4 : a.dim <= 128 ? 8 : 16;
+    const bool two = a.dim > 32 && (a.rotary == 0 || a.interleaved || a.rotary <= lpr * 8 || a.rotary == lpr * 16);
+    if (a.dim <= 32) return launch_shape<T, 4, 1>(a, stream);
+    if (a.dim <= 64) return two ? launch_shape<T, 4, 2>(a, stream) : launch_shape<T, 8, 1>(a, stream);
+    if (a.dim <= 128) return two ? launch_shape<T, 8, 2>(a, stream) : launch_shape<T, 16, 1>(a, stream);
+    return two ? launch_shape<T, 16, 2>(a, stream) : launch_shape<T, 32, 1>(a, stream);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -236,7 +284,7 @@ extern "C" onela_status onela_norm_rotate(const onela_norm_rotate_args* g, void*
             if (share_bytes(set[i], set[o])) return ONELA_E_INVAL;
         }
     NormArgs a{g->q_dev, g->k_dev, g->q_out_dev, g->k_out_dev, nullptr, nullptr, g->positions_dev, g->inv_freq_dev, g->q_stride, g->k_stride, g->q_out_stride, g->k_out_stride,
-               g->n_tokens, g->num_q_heads, g->num_q_heads + g->num_k_heads, g->head_dim, g->rotary_dim, g->interleaved != 0, g->norm, g->eps, g->q_scale, 1.f / (float)g->head_dim, 1, 0};
+               g->n_tokens, g->num_q_heads, g->num_q_heads + g->num_k_heads, g->head_dim, g->rotary_dim, g->interleaved != 0, g->norm, g->eps, g->q_scale, g->norm == ONELA_NORM_RMS ? 1.f / (float)g->head_dim : 1.f, 1, 0};
     if (g->norm == ONELA_NORM_RMS) {
         a.q_weight = g->q_weight_dev;
         a.k_weight = g->k_weight_dev;
