@@ -6,13 +6,14 @@
 // indices, passes uniform * sum.
 //
 // A row lies in the shared memory of one cluster of 1 to 8 CTAs, read from memory once.  Masses are integers, w in units of 2^-F with F = 62 -
-// ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included; w itself comes from 64-bit arithmetic.
+// ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included.  w = 2^y: y in 64 bits as a fixed-point number of 32
+// places, its fraction's upper 8 bits through a table, the rest through the exponential series (Tang 1989), 32 significant bits in all (by 64-bit exp():
+// 64 rows of 100 003 logits 132 us against MEASURED).
 //   top-k   tokens counted by bins of their distance from the largest (1024 bins); the bin in which the count passes k is cut
-//           into 1024 bins of the values' bit patterns, and so on until a bin holds one token or one value: three rounds at the most from 2^20
-//           different values, four from any
+//           into 1024 bins of the values' bit patterns, and so on until a bin holds one token or one value
 //   top-p   the same descent on the bins' masses, from the same first histogram, towards top_p times the mass of the top-k tokens
 // A histogram is reduced by the cluster (a CTA sums a share of the bins over all CTAs and hands the sums to all), two cluster barriers.
-// What bounds it: launches of a few rows the chain of barriers, many rows the 64-bit exponentials and the histogram's atomics.
+// What bounds it: launches of a few rows the chain of barriers, many rows the exponentials' and the histogram's instructions.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -28,7 +29,7 @@ namespace {
 namespace cg = cooperative_groups;
 using u64 = unsigned long long;
 
-constexpr int MAX_THREADS = 512, BINS = 1024, MAX_SLICE = 45056, MAX_CLUSTER = 8, MAX_VOCAB = 360000;
+constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 1024, MAX_SLICE = 45056, MAX_CLUSTER = 8, MAX_VOCAB = 360000;
 constexpr float BINS_PER_UNIT = 32.f;            // first histogram: bins of 1 / 32 up to 32 below the largest, the rest in the last one
 
 struct SampleArgs {
@@ -51,24 +52,30 @@ struct Histograms {                              // of one round, and what the c
 // What every CTA of a row knows.
 struct Row {
     float largest;
-    double inverse_t;
-    double unit;                                 // 2^F
+    double places;                               // log2(e) / T in units of 2^-32
+    int shift;                                   // F - 31
     bool greedy;
 };
 
 // bit pattern in the order of the values (-0 has been made +0, NaN -inf)
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t u = __float_as_uint(x);
-    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    const uint32_t u = __float_as_uint(x), k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return sizeof(T) == 2 ? k >> 16 : k;         // (bf16: the lower half says nothing)
 }
 __device__ __forceinline__ int first_bin(const Row& r, float x) { return min(BINS - 1, (int)((r.largest - x) * BINS_PER_UNIT)); }
-// the weight: 1 at the largest, 0 at -inf
-__device__ __forceinline__ double weight(const Row& r, float x) {
-    if (x == r.largest) return 1.0;
-    const double d = (double)x - (double)r.largest;
-    return isinf(d) ? 0.0 : exp(d * r.inverse_t);
+// The weight in units of 2^-F: 2^F at the largest, 0 at -inf.  table[j] = 2^(31 + j / 256).
+__device__ __forceinline__ u64 mass(const Row& r, const uint32_t* table, float x) {
+    if (x == r.largest) return 1ull << (r.shift + 31);
+    const long long y = __double2ll_rn(((double)x - (double)r.largest) * r.places);     // (saturates; T = inf: NaN at -inf, 0)
+    const int shift = r.shift + (int)(y >> 32);
+    const uint32_t part = (uint32_t)y;
+    if (shift < -31 || x == -INFINITY) return 0;
+    const float z = (float)(part & 0xffffffu) * 0x1.62e43p-33f;                         // ln 2 x 2^-32
+    const uint32_t e = __float2uint_rn(z * fmaf(z, fmaf(z, 1.f / 6.f, 0.5f), 1.f) * 0x1p40f);
+    const uint32_t t = table[part >> 24], w = t + (__umulhi(t, e) >> 8);
+    return shift >= 0 ? (u64)w << shift : (u64)(w >> -shift);
 }
-__device__ __forceinline__ u64 mass(const Row& r, double w) { return __double2ull_rn(w * r.unit); }
 
 // The end of the kept run: tokens of first bin `bin` whose keys lie in [low, high] are its last ones, `ties` of them (by index) kept; what
 // lies above is kept whole.
@@ -77,11 +84,12 @@ struct Cut {
     uint32_t low, high, ties;
 };
 // 1 above, 0 at the end of the run, -1 below
+template <typename T>
 __device__ __forceinline__ int side(const Row& r, const Cut& c, float x) {
     if (c.bin < 0) return 1;
     const int b = first_bin(r, x);
     if (b != c.bin) return b < c.bin ? 1 : -1;
-    const uint32_t k = key_of(x);
+    const uint32_t k = key_of<T>(x);
     return k > c.high ? 1 : k >= c.low ? 0 : -1;
 }
 
@@ -110,6 +118,7 @@ template <typename T>
 __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a) {
     constexpr int VE = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ uint32_t table_s[TABLE];
     __shared__ u64 scan64_s[MAX_THREADS / 32];
     __shared__ uint32_t scan32_s[MAX_THREADS / 32];
     __shared__ float largest_s, warp_largest_s[MAX_THREADS / 32];
@@ -127,6 +136,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     };
     Histograms* hist = reinterpret_cast<Histograms*>(smem);
     float* x_s = reinterpret_cast<float*>(smem + (a.histograms ? sizeof(Histograms) : 0));
+    for (int j = tid; j < TABLE; j += threads) table_s[j] = (uint32_t)__double2uint_rn(exp2(31.0 + j * (1.0 / TABLE)));
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -176,12 +186,14 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     for (int c = 0; c < ctas; ++c) r.largest = fmaxf(r.largest, *cluster.map_shared_rank(&largest_s, c));
     const float t = a.temperature ? a.temperature[row] : 1.f;
     r.greedy = !(t > 0.f);
-    r.inverse_t = 1.0 / (double)t;
-    r.unit = exp2((double)a.places);
+    const double inverse_t = 1.0 / (double)t;
+    r.places = inverse_t * (1.4426950408889634074 * 4294967296.0);
+    r.shift = a.places - 31;
     const int k = a.top_k ? a.top_k[row] : 0;
     const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p_given = a.min_p ? a.min_p[row] : 0.f;
     const bool use_k = k >= 1 && k < a.vocab, use_p = top_p < 1.f;
-    const double min_p = min_p_given > 0.f ? fmin((double)min_p_given, 1.0) : 0.0;
+    const double unit = (double)(1ull << a.places);
+    const u64 least = min_p_given > 0.f ? (u64)ceil(fmin((double)min_p_given, 1.0) * unit) : 1;     // (at least one unit: what has none is never drawn)
     const bool nothing = r.largest == -INFINITY;
 
     // ---- a histogram of the slice's tokens, summed over the cluster into all_*[which] ----
@@ -209,10 +221,10 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         for (int b = tid; b < BINS; b += threads) hist->count[b] = hist->low[b] = hist->high[b] = 0;
         __syncthreads();
     };
-    auto add = [&](int b, float x, bool masses) {
-        atomicAdd(&hist->count[b], 1u);
+    auto add = [&](int b, float x, bool counts, bool masses) {
+        if (counts) atomicAdd(&hist->count[b], 1u);
         if (!masses) return;
-        const u64 m = mass(r, weight(r, x));
+        const u64 m = mass(r, table_s, x);
         if (m == 0) return;
         const uint32_t low = (uint32_t)m, old = atomicAdd(&hist->low[b], low);
         const uint32_t high = (uint32_t)(m >> 32) + (old + low < old);
@@ -248,25 +260,30 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     // From the first histogram (all_*[0]) down to the end of the run; *kept_mass: the run's mass (with masses).
     auto descend = [&](bool by_mass, uint32_t want, double target, bool masses, u64* kept_mass) {
         find(0, by_mass, want, target, 0, 0);
-        Cut c{found_bin_s, 0u, 0xffffffffu, 0u};
+        Cut c{found_bin_s, 0u, key_of<T>(INFINITY), 0u};
         // keys that the bin can hold, half a bin more on either side (the bin of a value is off by far less)
         if (c.bin < BINS - 1) {
-            c.low = key_of((float)((double)r.largest - (c.bin + 1.5) / BINS_PER_UNIT));
-            c.high = key_of((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
+            c.low = key_of<T>((float)((double)r.largest - (c.bin + 1.5) / BINS_PER_UNIT));
+            c.high = key_of<T>((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
         } else {
-            c.high = key_of((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
+            c.high = key_of<T>((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
         }
-        if (isinf(r.largest)) { c.low = 0u; c.high = 0xffffffffu; }
+        if (isinf(r.largest)) {
+            c.low = 0u;
+            c.high = key_of<T>(INFINITY);
+        }
         uint32_t count = found_count_s, before = found_before_count_s;
+        bool counted = use_k;                                                      // (the first histogram counts for top-k only)
         u64 m = found_mass_s, mass_before = found_before_mass_s;
-        while (count > 1 && c.low != c.high) {
+        while (!counted || (count > 1 && c.low != c.high)) {
+            counted = true;
             const uint32_t range = c.high - c.low;                                 // bins of 2^shift keys, from the largest down
             const int shift = range < BINS ? 0 : 32 - __clz(range) - 10;
             clear();
             for (int j = tid; j < n; j += threads) {
                 const float x = x_s[j];
-                const uint32_t key = key_of(x);
-                if (first_bin(r, x) == c.bin && key >= c.low && key <= c.high) add((int)((c.high - key) >> shift), x, masses);
+                const uint32_t key = key_of<T>(x);
+                if (first_bin(r, x) == c.bin && key >= c.low && key <= c.high) add((int)((c.high - key) >> shift), x, true, masses);
             }
             reduce(1);
             find(1, by_mass, want, target, before, mass_before);
@@ -298,7 +315,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     Cut cut{-1, 0u, 0u, 0u};
     if (!nothing && !r.greedy && (use_k || use_p)) {
         clear();
-        for (int j = tid; j < n; j += threads) add(first_bin(r, x_s[j]), x_s[j], use_p);
+        for (int j = tid; j < n; j += threads) add(first_bin(r, x_s[j]), x_s[j], use_k, use_p);
         reduce(0);
         u64 kept;
         if (use_k) {
@@ -318,12 +335,10 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     // ---- the draw: thread = L consecutive tokens (L odd: no bank conflicts) ----
     const int L = ((n + threads - 1) / threads) | 1, begin = min(n, tid * L), stop = min(n, begin + L);
     auto kept_side = [&](float x, u64* m) {                                        // side() with min-p, and the mass
-        int s = r.greedy ? (x == r.largest ? 0 : -1) : side(r, cut, x);
+        const int s = r.greedy ? (x == r.largest ? 0 : -1) : side<T>(r, cut, x);
         if (s < 0) return -1;
-        const double w = weight(r, x);
-        if (w < min_p || w == 0.0) return -1;
-        *m = mass(r, w);
-        return s;
+        *m = mass(r, table_s, x);
+        return *m >= least ? s : -1;
     };
     const uint32_t ties = r.greedy ? 1u : cut.ties;
     u64 sum = 0, tie_mass = 0;
@@ -376,18 +391,38 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         const u64 target = min((u64)wanted, whole - 1);
         u64 m0 = cta_before + sum_before;
         uint32_t t0 = cta_ties_before + ties_before;
-        if (running(m0, t0) <= target && target < running(m0 + sum, t0 + tie_count)) {
-            for (int j = begin; j < stop; ++j) {
-                u64 m;
-                const int s = kept_side(x_s[j], &m);
-                if (s > 0) m0 += m;
-                else if (s == 0) ++t0;
-                if (target < running(m0, t0)) {
-                    a.tokens[row] = (int32_t)((long long)unit0 * VE + j - skip);
-                    if (a.logprobs)
-                        a.logprobs[row] = r.greedy ? 0.f : (float)((x_s[j] == r.largest ? 0.0 : ((double)x_s[j] - (double)r.largest) * r.inverse_t) - log((double)whole / r.unit));
+        const uint32_t here = __ballot_sync(0xffffffffu, running(m0, t0) <= target && target < running(m0 + sum, t0 + tie_count));
+        if (here) {                                                                // the warp goes through the one thread's tokens
+            const int lane = tid & 31, owner = __ffs(here) - 1;
+            m0 = __shfl_sync(0xffffffffu, m0, owner);
+            t0 = __shfl_sync(0xffffffffu, t0, owner);
+            const int first = __shfl_sync(0xffffffffu, begin, owner), last = __shfl_sync(0xffffffffu, stop, owner);
+            for (int j0 = first; j0 < last; j0 += 32) {
+                const int j = j0 + lane;
+                u64 m = 0;
+                const int s = j < last ? kept_side(x_s[j], &m) : -1;
+                u64 run = s > 0 ? m : 0;
+                uint32_t count = s == 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 y = __shfl_up_sync(0xffffffffu, run, o);
+                    const uint32_t c = __shfl_up_sync(0xffffffffu, count, o);
+                    if (lane >= o) {
+                        run += y;
+                        count += c;
+                    }
+                }
+                const uint32_t past = __ballot_sync(0xffffffffu, target < running(m0 + run, t0 + count));
+                if (past) {
+                    if (lane == __ffs(past) - 1) {
+                        a.tokens[row] = (int32_t)((long long)unit0 * VE + j - skip);
+                        if (a.logprobs)
+                            a.logprobs[row] = r.greedy ? 0.f : (float)((x_s[j] == r.largest ? 0.0 : ((double)x_s[j] - (double)r.largest) * inverse_t) - log((double)whole / unit));
+                    }
                     break;
                 }
+                m0 += __shfl_sync(0xffffffffu, run, 31);
+                t0 += __shfl_sync(0xffffffffu, count, 31);
             }
         }
     }
@@ -418,7 +453,7 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t stream) {
     const size_t smem = (size_t)((units + ctas - 1) / ctas) * VE * 4 + (a.histograms ? sizeof(Histograms) : 0);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * ctas));
-    cfg.blockDim = dim3(a.vocab / ctas > 4096 ? MAX_THREADS : 128);
+    cfg.blockDim = dim3(a.vocab / ctas > 16384 ? 1024 : a.vocab / ctas > 4096 ? 512 : 128);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
