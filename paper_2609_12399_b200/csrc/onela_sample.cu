@@ -6,9 +6,8 @@
 // indices, passes uniform * sum.
 //
 // A row lies in the shared memory of one cluster of 1 to 8 CTAs, read from memory once.  Masses are integers, w in units of 2^-F with F = 62 -
-// ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included.  w = 2^y: y in 64 bits as a fixed-point number of 32
-// places, its fraction's upper 8 bits through a table, the rest through the exponential series (Tang 1989), 32 significant bits in all (by 64-bit exp():
-// 64 rows of 100 003 logits 132 us against MEASURED).
+// ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included.  w = 2^(n / 256 + f / 256) in 64 bits, |f| <= 1 / 2:
+// 2^(n mod 256 / 256) from a table, the rest by its series to the third power (Tang 1989; relative error 2e-13): a third of the instructions of exp().
 //   top-k   tokens counted by bins of their distance from the largest (1024 bins); the bin in which the count passes k is cut
 //           into 1024 bins of the values' bit patterns, and so on until a bin holds one token or one value
 //   top-p   the same descent on the bins' masses, from the same first histogram, towards top_p times the mass of the top-k tokens
@@ -17,6 +16,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 
@@ -51,9 +51,9 @@ struct Histograms {                              // of one round, and what the c
 
 // What every CTA of a row knows.
 struct Row {
-    float largest;
-    double places;                               // log2(e) / T in units of 2^-32
-    int shift;                                   // F - 31
+    float largest, zero_from;                    // what lies below zero_from has no mass
+    double scale, offset;                        // 256 log2(e) / T, and the same times - largest
+    int places;                                  // F
     bool greedy;
 };
 
@@ -64,17 +64,14 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return sizeof(T) == 2 ? k >> 16 : k;         // (bf16: the lower half says nothing)
 }
 __device__ __forceinline__ int first_bin(const Row& r, float x) { return min(BINS - 1, (int)((r.largest - x) * BINS_PER_UNIT)); }
-// The weight in units of 2^-F: 2^F at the largest, 0 at -inf.  table[j] = 2^(31 + j / 256).
-__device__ __forceinline__ u64 mass(const Row& r, const uint32_t* table, float x) {
-    if (x == r.largest) return 1ull << (r.shift + 31);
-    const long long y = __double2ll_rn(((double)x - (double)r.largest) * r.places);     // (saturates; T = inf: NaN at -inf, 0)
-    const int shift = r.shift + (int)(y >> 32);
-    const uint32_t part = (uint32_t)y;
-    if (shift < -31 || x == -INFINITY) return 0;
-    const float z = (float)(part & 0xffffffu) * 0x1.62e43p-33f;                         // ln 2 x 2^-32
-    const uint32_t e = __float2uint_rn(z * fmaf(z, fmaf(z, 1.f / 6.f, 0.5f), 1.f) * 0x1p40f);
-    const uint32_t t = table[part >> 24], w = t + (__umulhi(t, e) >> 8);
-    return shift >= 0 ? (u64)w << shift : (u64)(w >> -shift);
+// The weight in units of 2^-F: 2^F at the largest, 0 at -inf.  table[j] = 2^(j / 256).
+__device__ __forceinline__ u64 mass(const Row& r, const double* table, float x) {
+    constexpr double MAGIC = 0x1.8p52, LN2 = 0x1.62e42fefa39efp-9;                      // (ln 2 / 256)
+    const double y = fma((double)x, r.scale, r.offset), t = y + MAGIC, f = (y - (t - MAGIC)) * LN2;
+    const int n = __double2loint(t);
+    const double w = table[n & (TABLE - 1)], v = fma(w, f * fma(f, fma(f, 1.0 / 6.0, 0.5), 1.0), w);
+    const u64 m = __double2ull_rn(__hiloint2double(__double2hiint(v) + ((n >> 8) + r.places) * (1 << 20), __double2loint(v)));
+    return x == r.largest ? 1ull << r.places : x < r.zero_from ? 0 : m;
 }
 
 // The end of the kept run: tokens of first bin `bin` whose keys lie in [low, high] are its last ones, `ties` of them (by index) kept; what
@@ -105,28 +102,30 @@ __device__ __forceinline__ X block_exclusive_scan(X x, X* warp_s, X* total) {
     __syncthreads();                             // warp_s is free
     if (lane == 31) warp_s[warp] = run;
     __syncthreads();
-    X before = 0, all = 0;
-    for (int w = 0; w < warps; ++w) {
-        if (w == warp) before = all;
-        all += warp_s[w];
+    const X own = lane < warps ? warp_s[lane] : 0;
+    X sum = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const X y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
     }
-    *total = all;
-    return before + run - x;
+    *total = __shfl_sync(0xffffffffu, sum, 31);
+    return __shfl_sync(0xffffffffu, sum - own, warp) + run - x;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a) {
     constexpr int VE = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ uint32_t table_s[TABLE];
+    __shared__ double table_s[TABLE];
     __shared__ u64 scan64_s[MAX_THREADS / 32];
     __shared__ uint32_t scan32_s[MAX_THREADS / 32];
     __shared__ float largest_s, warp_largest_s[MAX_THREADS / 32];
     __shared__ u64 total_mass_s, tie_mass_s;
     __shared__ uint32_t total_ties_s;
     __shared__ int found_bin_s;
-    __shared__ u64 found_mass_s, found_before_mass_s;
-    __shared__ uint32_t found_count_s, found_before_count_s;
+    __shared__ u64 found_mass_s, found_before_count_s, found_before_mass_s;
+    __shared__ uint32_t found_count_s;
     const cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, threads = blockDim.x;
     const long long row = blockIdx.x / ctas;
@@ -136,7 +135,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     };
     Histograms* hist = reinterpret_cast<Histograms*>(smem);
     float* x_s = reinterpret_cast<float*>(smem + (a.histograms ? sizeof(Histograms) : 0));
-    for (int j = tid; j < TABLE; j += threads) table_s[j] = (uint32_t)__double2uint_rn(exp2(31.0 + j * (1.0 / TABLE)));
+    for (int j = tid; j < TABLE; j += threads) table_s[j] = exp2(j * (1.0 / TABLE));
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -187,8 +186,11 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     const float t = a.temperature ? a.temperature[row] : 1.f;
     r.greedy = !(t > 0.f);
     const double inverse_t = 1.0 / (double)t;
-    r.places = inverse_t * (1.4426950408889634074 * 4294967296.0);
-    r.shift = a.places - 31;
+    r.places = a.places;
+    r.scale = inverse_t * (256.0 * 1.4426950408889634074);
+    r.offset = -(double)r.largest * r.scale;
+    // 2^(F + 1) of them make one unit.  (Where that lies below every float, or T is infinite: only -inf has none.)
+    r.zero_from = fmaxf((float)((double)r.largest - (a.places + 1) * 0.69314718055994530942 * (double)t), -FLT_MAX);
     const int k = a.top_k ? a.top_k[row] : 0;
     const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p_given = a.min_p ? a.min_p[row] : 0.f;
     const bool use_k = k >= 1 && k < a.vocab, use_p = top_p < 1.f;
@@ -230,20 +232,20 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         const uint32_t high = (uint32_t)(m >> 32) + (old + low < old);
         if (high) atomicAdd(&hist->high[b], high);
     };
-    // The bin of all_*[which] in which the count passes `want` (by_mass: the mass reaches `target`), and what lies before it.
-    auto find = [&](int which, bool by_mass, uint32_t want, double target, uint32_t count0, u64 mass0) {
+    // The bin of all_*[which] in which the count passes `want` (by_mass: the mass reaches `target`), and what lies before it (of the mass
+    // only where masses are kept, of the count only where it is what is looked for).
+    auto find = [&](int which, bool by_mass, bool masses, uint32_t want, double target, u64 count0, u64 mass0) {
         const int per = BINS / threads, at = tid * per;
-        uint32_t count = 0, all_count;
-        u64 m = 0, all_mass;
+        u64 count = 0, m = 0, all;
         for (int b = 0; b < per; ++b) {
             count += hist->all_count[which][at + b];
             m += hist->all_mass[which][at + b];
         }
-        uint32_t before = count0 + block_exclusive_scan<uint32_t>(count, scan32_s, &all_count);
-        u64 mass_before = mass0 + block_exclusive_scan<u64>(m, scan64_s, &all_mass);
+        u64 before = by_mass ? 0 : count0 + block_exclusive_scan<u64>(count, scan64_s, &all);
+        u64 mass_before = masses ? mass0 + block_exclusive_scan<u64>(m, scan64_s, &all) : 0;
         for (int b = 0; b < per; ++b) {
-            const uint32_t c = hist->all_count[which][at + b];
             const u64 w = hist->all_mass[which][at + b];
+            const uint32_t c = hist->all_count[which][at + b];
             const bool here = by_mass ? (double)mass_before < target && (double)(mass_before + w) >= target : before < want && before + c >= want;
             if (here) {
                 found_bin_s = at + b;
@@ -257,9 +259,19 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         }
         __syncthreads();
     };
+    // all tokens of the slice, four at a time
+    auto each_token = [&](auto f) {
+        for (int j = tid; j < n / 4; j += threads) {
+            const float4 x = *reinterpret_cast<const float4*>(x_s + 4 * j);
+            f(x.x);
+            f(x.y);
+            f(x.z);
+            f(x.w);
+        }
+    };
     // From the first histogram (all_*[0]) down to the end of the run; *kept_mass: the run's mass (with masses).
     auto descend = [&](bool by_mass, uint32_t want, double target, bool masses, u64* kept_mass) {
-        find(0, by_mass, want, target, 0, 0);
+        find(0, by_mass, masses, want, target, 0, 0);
         Cut c{found_bin_s, 0u, key_of<T>(INFINITY), 0u};
         // keys that the bin can hold, half a bin more on either side (the bin of a value is off by far less)
         if (c.bin < BINS - 1) {
@@ -272,21 +284,20 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             c.low = 0u;
             c.high = key_of<T>(INFINITY);
         }
-        uint32_t count = found_count_s, before = found_before_count_s;
+        uint32_t count = found_count_s;
         bool counted = use_k;                                                      // (the first histogram counts for top-k only)
-        u64 m = found_mass_s, mass_before = found_before_mass_s;
+        u64 m = found_mass_s, before = found_before_count_s, mass_before = found_before_mass_s;
         while (!counted || (count > 1 && c.low != c.high)) {
             counted = true;
             const uint32_t range = c.high - c.low;                                 // bins of 2^shift keys, from the largest down
             const int shift = range < BINS ? 0 : 32 - __clz(range) - 10;
             clear();
-            for (int j = tid; j < n; j += threads) {
-                const float x = x_s[j];
+            each_token([&](float x) {
                 const uint32_t key = key_of<T>(x);
-                if (first_bin(r, x) == c.bin && key >= c.low && key <= c.high) add((int)((c.high - key) >> shift), x, true, masses);
-            }
+                if (key - c.low <= range && first_bin(r, x) == c.bin) add((int)((c.high - key) >> shift), x, true, masses);
+            });
             reduce(1);
-            find(1, by_mass, want, target, before, mass_before);
+            find(1, by_mass, masses, want, target, before, mass_before);
             const uint32_t top = c.high - ((uint32_t)found_bin_s << shift), span = (1u << shift) - 1;
             c.low = top - c.low > span ? top - span : c.low;
             c.high = top;
@@ -306,7 +317,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             }
             c.ties = low;
         } else {
-            c.ties = want - before;
+            c.ties = want - (uint32_t)before;
         }
         *kept_mass = mass_before + c.ties * one;
         return c;
@@ -315,9 +326,10 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     Cut cut{-1, 0u, 0u, 0u};
     if (!nothing && !r.greedy && (use_k || use_p)) {
         clear();
-        for (int j = tid; j < n; j += threads) add(first_bin(r, x_s[j]), x_s[j], use_k, use_p);
+        if (use_p) each_token([&](float x) { add(first_bin(r, x), x, use_k, true); });
+        else each_token([&](float x) { add(first_bin(r, x), x, true, false); });
         reduce(0);
-        u64 kept;
+        u64 kept = 0;
         if (use_k) {
             cut = descend(false, (uint32_t)k, 0.0, use_p, &kept);
         } else {
