@@ -10,7 +10,9 @@
 // 2^(n mod 256 / 256) from a table, the rest by its series to the third power (Tang 1989; relative error 2e-13): a third of the instructions of exp().
 //   top-k   tokens counted by bins of their distance from the largest (1024 bins); the bin in which the count passes k is cut
 //           into 1024 bins of the values' bit patterns, and so on until a bin holds one token or one value
-//   top-p   the same descent on the bins' masses, from the same first histogram, towards top_p times the mass of the top-k tokens
+//   top-p   the same counts times the bins' weights say near which bin the mass reaches top_p times that of the top-k tokens; the exact mass before
+//           that bin and in it and its neighbours (sums in registers; a bisection if it was none of them) says which, and the bin is cut by masses as above.
+//           (Exact masses per bin from the start are two more atomics per token, which return: 64 rows of 100 003 logits 81 us against MEASURED.)
 // A histogram is reduced by the cluster (a CTA sums a share of the bins over all CTAs and hands the sums to all), two cluster barriers.
 // What bounds it: launches of a few rows the chain of barriers, many rows the exponentials' and the histogram's instructions.
 #include <cooperative_groups.h>
@@ -29,7 +31,7 @@ namespace {
 namespace cg = cooperative_groups;
 using u64 = unsigned long long;
 
-constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 1024, MAX_SLICE = 45056, MAX_CLUSTER = 8, MAX_VOCAB = 360000;
+constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 1024, FINE = 512, MAX_SLICE = 51712, MAX_CLUSTER = 8, WINDOW = 16, MAX_VOCAB = 360000;
 constexpr float BINS_PER_UNIT = 32.f;            // first histogram: bins of 1 / 32 up to 32 below the largest, the rest in the last one
 
 struct SampleArgs {
@@ -43,10 +45,18 @@ struct SampleArgs {
     int32_t histograms;                          // shared memory has room for them
 };
 
-struct Histograms {                              // of one round, and what the cluster made of the first and of the current one
-    uint32_t count[BINS], low[BINS], high[BINS];
-    uint32_t all_count[2][BINS];
-    u64 all_mass[2][BINS];
+// The first histogram has BINS bins and counts, finer ones FINE bins and masses too.  (As small as this so that two CTAs hold 103 000 fp32
+// logits: by four 64 rows are two waves.)
+struct Histograms {
+    uint32_t count[BINS], low[FINE], high[FINE];      // this CTA's; a mass's two halves
+    uint32_t all_count[BINS];                         // the cluster's first one
+    union {
+        struct {
+            u64 mass[FINE];
+            uint32_t count[FINE];
+        } fine;                                       // the cluster's finer one
+        float queue[MAX_THREADS / 32][64];            // of each_token_from, before the others may write `fine`
+    };
 };
 
 // What every CTA of a row knows.
@@ -75,19 +85,24 @@ __device__ __forceinline__ u64 mass(const Row& r, const double* table, float x) 
 }
 
 // The end of the kept run: tokens of first bin `bin` whose keys lie in [low, high] are its last ones, `ties` of them (by index) kept; what
-// lies above is kept whole.
+// lies above is kept whole.  No token of the bin lies outside [from, to].
 struct Cut {
     int bin;                                     // -1: everything is above
+    float from, to;
     uint32_t low, high, ties;
 };
+// values that a bin can hold, half a bin more on either side (the bin of a value is off by far less)
+__device__ __forceinline__ float bin_from(const Row& r, int b) {
+    return b >= BINS - 1 || isinf(r.largest) ? -INFINITY : (float)((double)r.largest - (b + 1.5) / BINS_PER_UNIT);
+}
+__device__ __forceinline__ float bin_to(const Row& r, int b) { return isinf(r.largest) ? INFINITY : (float)((double)r.largest - (b - 0.5) / BINS_PER_UNIT); }
 // 1 above, 0 at the end of the run, -1 below
 template <typename T>
 __device__ __forceinline__ int side(const Row& r, const Cut& c, float x) {
-    if (c.bin < 0) return 1;
     const int b = first_bin(r, x);
-    if (b != c.bin) return b < c.bin ? 1 : -1;
     const uint32_t k = key_of<T>(x);
-    return k > c.high ? 1 : k >= c.low ? 0 : -1;
+    const int within = k > c.high ? 1 : k >= c.low ? 0 : -1;
+    return c.bin < 0 || b < c.bin ? 1 : b > c.bin ? -1 : within;
 }
 
 template <typename X>
@@ -122,9 +137,13 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     __shared__ uint32_t scan32_s[MAX_THREADS / 32];
     __shared__ float largest_s, warp_largest_s[MAX_THREADS / 32];
     __shared__ u64 total_mass_s, tie_mass_s;
-    __shared__ uint32_t total_ties_s;
+    __shared__ uint32_t total_ties_s, run_ties_s[32];
+    __shared__ u64 run_sum_s[32], run_tie_mass_s[32];
+    __shared__ int run_found_s;
     __shared__ int found_bin_s;
-    __shared__ u64 found_mass_s, found_before_count_s, found_before_mass_s;
+    __shared__ u64 found_mass_s, found_before_s;
+    __shared__ float scanf_s[MAX_THREADS / 32];
+    __shared__ u64 part_s[MAX_THREADS / 32][4], cta_part_s[2][4], row_part_s[4];
     __shared__ uint32_t found_count_s;
     const cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, threads = blockDim.x;
@@ -147,22 +166,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     const int unit0 = min(units, rank * each), n = (min(units, unit0 + each) - unit0) * VE;
     const T* base = p - skip;
     float best = -INFINITY;
-#pragma unroll 4
-    for (int u = tid; u < n / VE; u += threads) {
-        const long long at = (long long)(unit0 + u) * VE;
-        float x[VE];
-        if (at >= skip && at + VE <= end) {
-            Vec16<T>::load(base + at, x);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                x[e] = -INFINITY;
-                if (at + e >= skip && at + e < end) {
-                    if constexpr (sizeof(T) == 2) x[e] = __bfloat162float(base[at + e]);
-                    else x[e] = base[at + e];
-                }
-            }
-        }
+    auto take = [&](int u, float* x) {                                             // (NaN: as -inf, -0: as +0)
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             x[e] = x[e] == x[e] ? x[e] + 0.f : -INFINITY;
@@ -170,6 +174,39 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         }
 #pragma unroll
         for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4*>(x_s + u * VE + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+    };
+    // whole vectors, eight on their way at a time; the row's first and last one by elements
+    const int whole0 = unit0 == 0 && skip > 0 ? 1 : 0, whole1 = n / VE - (unit0 + n / VE == units && end % VE != 0 ? 1 : 0);
+    constexpr int BATCH = 8;
+    for (int u0 = whole0 + tid; u0 < whole1; u0 += threads * BATCH) {
+        uint4 raw[BATCH];
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            const int u = u0 + e * threads;
+            if (u < whole1) raw[e] = __ldg(reinterpret_cast<const uint4*>(base) + unit0 + u);
+        }
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            const int u = u0 + e * threads;
+            if (u >= whole1) break;
+            float x[VE];
+            Vec16<T>::unpack(raw[e], x);
+            take(u, x);
+        }
+    }
+    const int edge = tid == 0 && whole0 > 0 ? 0 : tid == 1 && whole1 < n / VE && (whole1 > 0 || whole0 == 0) ? whole1 : -1;
+    if (edge >= 0) {
+        const long long at = (long long)(unit0 + edge) * VE;
+        float x[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            x[e] = -INFINITY;
+            if (at + e >= skip && at + e < end) {
+                if constexpr (sizeof(T) == 2) x[e] = __bfloat162float(base[at + e]);
+                else x[e] = base[at + e];
+            }
+        }
+        take(edge, x);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
@@ -199,67 +236,97 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     const bool nothing = r.largest == -INFINITY;
 
     // ---- a histogram of the slice's tokens, summed over the cluster into all_*[which] ----
-    auto reduce = [&](int which) {
+    auto reduce_first = [&] {
         sync();
         const int share = BINS / ctas;
         for (int b = tid; b < share; b += threads) {
             const int at = rank * share + b;
-            uint32_t count = 0;
+            uint32_t count[MAX_CLUSTER], all = 0;
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c) count[c] = c < ctas ? cluster.map_shared_rank(hist, c)->count[at] : 0;
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c) all += count[c];
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < ctas) cluster.map_shared_rank(hist, c)->all_count[at] = all;
+        }
+        sync();
+    };
+    auto reduce_fine = [&](bool masses) {
+        sync();
+        const int share = FINE / ctas;
+        for (int b = tid; b < share; b += threads) {
+            const int at = rank * share + b;
+            uint32_t count[MAX_CLUSTER], low[MAX_CLUSTER], high[MAX_CLUSTER];
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c) {
+                count[c] = low[c] = high[c] = 0;
+                if (c < ctas) {
+                    const Histograms* h = cluster.map_shared_rank(hist, c);
+                    count[c] = h->count[at];
+                    if (masses) {
+                        low[c] = h->low[at];
+                        high[c] = h->high[at];
+                    }
+                }
+            }
+            uint32_t all = 0;
             u64 m = 0;
-            for (int c = 0; c < ctas; ++c) {
-                const Histograms* h = cluster.map_shared_rank(hist, c);
-                count += h->count[at];
-                m += (u64)h->low[at] | (u64)h->high[at] << 32;
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c) {
+                all += count[c];
+                m += (u64)low[c] | (u64)high[c] << 32;
             }
-            for (int c = 0; c < ctas; ++c) {
-                Histograms* h = cluster.map_shared_rank(hist, c);
-                h->all_count[which][at] = count;
-                h->all_mass[which][at] = m;
-            }
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < ctas) {
+                    Histograms* h = cluster.map_shared_rank(hist, c);
+                    h->fine.count[at] = all;
+                    h->fine.mass[at] = m;
+                }
         }
         sync();
     };
     auto clear = [&] {
-        for (int b = tid; b < BINS; b += threads) hist->count[b] = hist->low[b] = hist->high[b] = 0;
+        for (int b = tid; b < BINS; b += threads) hist->count[b] = 0;
+        for (int b = tid; b < FINE; b += threads) hist->low[b] = hist->high[b] = 0;
         __syncthreads();
     };
-    auto add = [&](int b, float x, bool counts, bool masses) {
-        if (counts) atomicAdd(&hist->count[b], 1u);
-        if (!masses) return;
-        const u64 m = mass(r, table_s, x);
+    auto add = [&](int b, u64 m) {
+        atomicAdd(&hist->count[b], 1u);
         if (m == 0) return;
         const uint32_t low = (uint32_t)m, old = atomicAdd(&hist->low[b], low);
         const uint32_t high = (uint32_t)(m >> 32) + (old + low < old);
         if (high) atomicAdd(&hist->high[b], high);
     };
-    // The bin of all_*[which] in which the count passes `want` (by_mass: the mass reaches `target`), and what lies before it (of the mass
-    // only where masses are kept, of the count only where it is what is looked for).
-    auto find = [&](int which, bool by_mass, bool masses, uint32_t want, double target, u64 count0, u64 mass0) {
-        const int per = BINS / threads, at = tid * per;
-        u64 count = 0, m = 0, all;
-        for (int b = 0; b < per; ++b) {
-            count += hist->all_count[which][at + b];
-            m += hist->all_mass[which][at + b];
-        }
-        u64 before = by_mass ? 0 : count0 + block_exclusive_scan<u64>(count, scan64_s, &all);
-        u64 mass_before = masses ? mass0 + block_exclusive_scan<u64>(m, scan64_s, &all) : 0;
-        for (int b = 0; b < per; ++b) {
-            const u64 w = hist->all_mass[which][at + b];
-            const uint32_t c = hist->all_count[which][at + b];
-            const bool here = by_mass ? (double)mass_before < target && (double)(mass_before + w) >= target : before < want && before + c >= want;
+    // The bin (of the first or a finer histogram) in which the count passes `want` (by_mass: the mass reaches `target`), and what of either lies
+    // before it.
+    auto find = [&](bool fine, bool by_mass, uint32_t want, double target, u64 base0) {
+        const int bins = fine ? FINE : BINS, per = max(1, bins / threads), at = tid * per;
+        auto count_of = [&](int b) { return fine ? hist->fine.count[b] : hist->all_count[b]; };
+        u64 sum = 0, all;
+        for (int b = at; b < min(bins, at + per); ++b) sum += by_mass ? hist->fine.mass[b] : count_of(b);
+        u64 before = base0 + block_exclusive_scan<u64>(sum, scan64_s, &all);
+        for (int b = at; b < min(bins, at + per); ++b) {
+            const u64 step = by_mass ? hist->fine.mass[b] : count_of(b);
+            const bool here = by_mass ? (double)before < target && (double)(before + step) >= target : before < want && before + step >= want;
             if (here) {
-                found_bin_s = at + b;
-                found_count_s = c;
-                found_mass_s = w;
-                found_before_count_s = before;
-                found_before_mass_s = mass_before;
+                found_bin_s = b;
+                found_count_s = count_of(b);
+                found_mass_s = fine ? hist->fine.mass[b] : 0;
+                found_before_s = before;
             }
-            before += c;
-            mass_before += w;
+            before += step;
         }
         __syncthreads();
     };
-    // all tokens of the slice, four at a time
+    // All tokens of the slice, four at a time: a warp has a run of neighbours.  (What works on a token has no branches: four tokens hide each
+    // other's latency.)
+    const int lane = tid & 31, run4 = ((n / 4 + threads / 32 - 1) / (threads / 32) + 31) & ~31, first4 = (tid >> 5) * run4;      // in fours
+    auto fours = [&](auto f) {
+        for (int i = lane; i < run4; i += 32)
+            f(first4 + i < n / 4 ? *reinterpret_cast<const float4*>(x_s + 4 * (first4 + i)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY));
+    };
     auto each_token = [&](auto f) {
         for (int j = tid; j < n / 4; j += threads) {
             const float4 x = *reinterpret_cast<const float4*>(x_s + 4 * j);
@@ -269,126 +336,283 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             f(x.w);
         }
     };
-    // From the first histogram (all_*[0]) down to the end of the run; *kept_mass: the run's mass (with masses).
-    auto descend = [&](bool by_mass, uint32_t want, double target, bool masses, u64* kept_mass) {
-        find(0, by_mass, masses, want, target, 0, 0);
-        Cut c{found_bin_s, 0u, key_of<T>(INFINITY), 0u};
-        // keys that the bin can hold, half a bin more on either side (the bin of a value is off by far less)
-        if (c.bin < BINS - 1) {
-            c.low = key_of<T>((float)((double)r.largest - (c.bin + 1.5) / BINS_PER_UNIT));
-            c.high = key_of<T>((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
-        } else {
-            c.high = key_of<T>((float)((double)r.largest - (c.bin - 0.5) / BINS_PER_UNIT));
+    // The tokens from `from` up, in whole warps: what costs tens of instructions per token is not done for those below.
+    float* queue = hist->queue[tid >> 5];
+    auto each_token_from = [&](float from, auto f) {
+        int count = 0;
+        fours([&](float4 x4) {
+            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t mask = __ballot_sync(0xffffffffu, x[e] >= from);
+                if (x[e] >= from) queue[count + __popc(mask & ((1u << lane) - 1))] = x[e];
+                count += __popc(mask);
+                if (count >= 32) {
+                    __syncwarp();
+                    count -= 32;
+                    f(queue[count + lane]);
+                    __syncwarp();
+                }
+            }
+        });
+        __syncwarp();
+        if (count > 0) f(lane < count ? queue[lane] : -INFINITY);
+    };
+    // Four sums over the threads of the whole cluster, in row_part_s
+    int flip = 0;
+    auto sum_over_row = [&](u64 v0, u64 v1, u64 v2, u64 v3) {
+        u64 v[4] = {v0, v1, v2, v3};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v[e] += __shfl_xor_sync(0xffffffffu, v[e], o);
+            if ((tid & 31) == 0) part_s[tid >> 5][e] = v[e];
         }
-        if (isinf(r.largest)) {
-            c.low = 0u;
-            c.high = key_of<T>(INFINITY);
+        __syncthreads();
+        if (tid < 4) {
+            u64 x = 0;
+            for (int w = 0; w < threads / 32; ++w) x += part_s[w][tid];
+            cta_part_s[flip][tid] = x;
         }
-        uint32_t count = found_count_s;
-        bool counted = use_k;                                                      // (the first histogram counts for top-k only)
-        u64 m = found_mass_s, before = found_before_count_s, mass_before = found_before_mass_s;
-        while (!counted || (count > 1 && c.low != c.high)) {
-            counted = true;
+        sync();
+        if (tid < 32) {                                                            // lane: CTA tid / 4, sum tid % 4
+            u64 x = (tid >> 2) < ctas ? *cluster.map_shared_rank(&cta_part_s[flip][tid & 3], tid >> 2) : 0;
+#pragma unroll
+            for (int o = 16; o > 2; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            if (tid < 4) row_part_s[tid] = x;
+        }
+        __syncthreads();
+        flip ^= 1;
+    };
+    // From bin `bin` of the first histogram, which holds `count` tokens, down to the end of the run: towards `want` tokens (by_mass: a mass of
+    // `target`), `before` of them (of it) in the bins above.
+    auto descend = [&](int bin, uint32_t count, bool by_mass, uint32_t want, double target, u64 before, u64 m) {
+        Cut c{bin, bin_from(r, bin), bin_to(r, bin), 0u, 0u, 0u};
+        c.low = key_of<T>(c.from);
+        c.high = key_of<T>(c.to);
+        while (count > 1 && c.low != c.high) {
             const uint32_t range = c.high - c.low;                                 // bins of 2^shift keys, from the largest down
-            const int shift = range < BINS ? 0 : 32 - __clz(range) - 10;
+            const int shift = range < FINE ? 0 : 32 - __clz(range) - 9;
             clear();
-            each_token([&](float x) {
-                const uint32_t key = key_of<T>(x);
-                if (key - c.low <= range && first_bin(r, x) == c.bin) add((int)((c.high - key) >> shift), x, true, masses);
+            fours([&](float4 x4) {
+                const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+                if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) < c.from) return;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t key = key_of<T>(x[e]);
+                    if (x[e] >= c.from && x[e] <= c.to && key - c.low <= range && first_bin(r, x[e]) == c.bin)
+                        add((int)((c.high - key) >> shift), by_mass ? mass(r, table_s, x[e]) : 0);
+                }
             });
-            reduce(1);
-            find(1, by_mass, masses, want, target, before, mass_before);
+            reduce_fine(by_mass);
+            find(true, by_mass, want, target, before);
             const uint32_t top = c.high - ((uint32_t)found_bin_s << shift), span = (1u << shift) - 1;
             c.low = top - c.low > span ? top - span : c.low;
             c.high = top;
             count = found_count_s;
-            before = found_before_count_s;
+            before = found_before_s;
             m = found_mass_s;
-            mass_before = found_before_mass_s;
             __syncthreads();                                                       // found_* may be written again
         }
-        const u64 one = count ? m / count : 0;                                     // tokens of one value have one mass
         if (by_mass) {
-            uint32_t low = 1, high = max(count, 1u);                               // the fewest that reach the target
+            const u64 one = m / count;                                             // tokens of one value have one mass
+            uint32_t low = 1, high = count;                                        // the fewest that reach the target
             while (low < high) {
                 const uint32_t mid = low + (high - low) / 2;
-                if ((double)(mass_before + mid * one) >= target) high = mid;
+                if ((double)(before + mid * one) >= target) high = mid;
                 else low = mid + 1;
             }
             c.ties = low;
         } else {
             c.ties = want - (uint32_t)before;
         }
-        *kept_mass = mass_before + c.ties * one;
         return c;
     };
 
-    Cut cut{-1, 0u, 0u, 0u};
+    Cut cut{-1, 0.f, 0.f, 0u, 0u, 0u};
     if (!nothing && !r.greedy && (use_k || use_p)) {
         clear();
-        if (use_p) each_token([&](float x) { add(first_bin(r, x), x, use_k, true); });
-        else each_token([&](float x) { add(first_bin(r, x), x, true, false); });
-        reduce(0);
-        u64 kept = 0;
+        u64 s0 = 0, s1 = 0;
+        uint32_t s2 = 0;
+        if (use_k) each_token([&](float x) { atomicAdd(&hist->count[first_bin(r, x)], 1u); });
+        else each_token([&](float x) {
+            atomicAdd(&hist->count[first_bin(r, x)], 1u);
+            s0 += mass(r, table_s, x);
+        });
+        reduce_first();
         if (use_k) {
-            cut = descend(false, (uint32_t)k, 0.0, use_p, &kept);
-        } else {
-            u64 part = 0;
-            for (int b = tid; b < BINS; b += threads) part += hist->all_mass[0][b];
-            block_exclusive_scan<u64>(part, scan64_s, &kept);
+            find(false, false, (uint32_t)k, 0.0, 0);
+            const int bin = found_bin_s;
+            const uint32_t count = found_count_s;
+            const u64 before = found_before_s;
+            __syncthreads();
+            cut = descend(bin, count, false, (uint32_t)k, 0.0, before, 0);
         }
         if (use_p) {
-            __syncthreads();
+            if (use_k)                                                             // masses above the cut and at it, tokens at it
+                each_token_from(cut.from, [&](float x) {
+                    const int s = side<T>(r, cut, x);
+                    const u64 m = s >= 0 ? mass(r, table_s, x) : 0;
+                    s0 += s > 0 ? m : 0;
+                    s1 += s == 0 ? m : 0;
+                    s2 += s == 0;
+                });
+            sum_over_row(s0, s1, s2, 0);
+            const u64 kept = row_part_s[0] + (row_part_s[2] ? row_part_s[1] / row_part_s[2] * cut.ties : 0);
             const double target = fmax((double)top_p * (double)kept, 0.5);         // (the largest is always kept)
-            cut = descend(true, 0u, target, true, &kept);
+            // near which bin: counts times the weights in the bins' middles, in proportion to a mass that is known (values that sit at one edge
+            // of their bins, as bf16 ones do, weigh a per cent more than that: a dozen bins)
+            const int per = BINS / threads, at = tid * per;
+            const float bin_scale = (float)(-r.scale / (256.0 * BINS_PER_UNIT));
+            auto guess = [&](int b) { return (float)hist->all_count[b] * exp2f((b + 0.5f) * bin_scale); };
+            float sum = 0.f, all;
+            for (int b = 0; b < per; ++b)
+                if (!use_k || at + b <= cut.bin) sum += guess(at + b);
+            const float guess_before = block_exclusive_scan<float>(sum, scanf_s, &all);
+            auto guess_bin = [&](float near) {                                     // the bin in which the guesses' sum passes `near`, -1: none
+                if (tid == 0) found_bin_s = -1;
+                __syncthreads();
+                float reached = guess_before;
+                for (int b = 0; b < per; ++b) {
+                    const float to = reached + guess(at + b);
+                    if (reached < near && to >= near) found_bin_s = at + b;
+                    reached = to;
+                }
+                __syncthreads();
+                const int bin = found_bin_s;
+                __syncthreads();
+                return bin;
+            };
+            int bin = guess_bin((float)(target / (double)max(kept, 1ull)) * all), lo = 0, hi = BINS - 1;      // the one that reaches the target lies in [lo, hi]
+            for (;;) {
+                // the exact mass before a window of bins around the guess, and in each of them
+                if (bin < lo || bin > hi) bin = (lo + hi) / 2;
+                const int b0 = max(lo, min(bin - WINDOW / 2, hi - (WINDOW - 1)));
+                u64 above = 0, inside = 0;
+                clear();
+                each_token_from(bin_from(r, b0 + WINDOW - 1), [&](float x) {
+                    const int b = first_bin(r, x) - b0;
+                    const u64 m = mass(r, table_s, x);
+                    above += b < 0 ? m : 0;
+                    if (b >= 0 && b < WINDOW && x > -INFINITY) {
+                        inside += m;
+                        add(b, m);
+                    }
+                });
+                sum_over_row(above, inside, 0, 0);
+                const u64 before = row_part_s[0];
+                if ((double)before < target && (double)(before + row_part_s[1]) >= target) {
+                    reduce_fine(true);
+                    find(true, true, 0u, target, before);
+                    bin = b0 + found_bin_s;
+                    const uint32_t count = found_count_s;
+                    const u64 before_bin = found_before_s, m = found_mass_s;
+                    __syncthreads();
+                    cut = descend(bin, count, true, 0u, target, before_bin, m);
+                    break;
+                }
+                if ((double)before >= target) hi = b0 - 1;
+                else lo = b0 + WINDOW;
+                if (b0 >= at && b0 < at + per) {                                   // again, in proportion to the mass before b0
+                    float reached = guess_before;
+                    for (int b = at; b < b0; ++b) reached += guess(b);
+                    scanf_s[0] = reached;
+                }
+                __syncthreads();
+                const float reached = scanf_s[0];
+                __syncthreads();
+                bin = guess_bin((float)(target / (double)max(before, 1ull)) * reached);
+            }
         }
     }
 
-    // ---- the draw: thread = L consecutive tokens (L odd: no bank conflicts) ----
-    const int L = ((n + threads - 1) / threads) | 1, begin = min(n, tid * L), stop = min(n, begin + L);
-    auto kept_side = [&](float x, u64* m) {                                        // side() with min-p, and the mass
-        const int s = r.greedy ? (x == r.largest ? 0 : -1) : side<T>(r, cut, x);
-        if (s < 0) return -1;
+    // ---- the draw: kept masses by warps (runs of neighbours), then the one run that passes the target token by token ----
+    // (a quick no for most: what lies below the cut's bin, or has no mass, or clearly less than min-p)
+    float floor_x = r.zero_from;
+    if (cut.bin >= 0) floor_x = fmaxf(floor_x, cut.from);
+    if (min_p_given > 0.f && t < INFINITY) floor_x = fmaxf(floor_x, (float)((double)r.largest + (double)t * (log(fmin((double)min_p_given, 1.0)) - 1e-3)) - fabsf(r.largest) * 0x1p-22f);
+    if (r.greedy) floor_x = r.largest;
+    // 1: kept, 0: a tie at the end of the run, -1: not kept; its mass, 0 where not kept
+    auto kept_side = [&](float x, u64* m) {
+        int s = r.greedy ? (x == r.largest ? 0 : -1) : side<T>(r, cut, x);
         *m = mass(r, table_s, x);
-        return *m >= least ? s : -1;
+        s = *m >= least ? s : -1;
+        *m = s >= 0 ? *m : 0;
+        return s;
     };
     const uint32_t ties = r.greedy ? 1u : cut.ties;
     u64 sum = 0, tie_mass = 0;
     uint32_t tie_count = 0;
+    auto tally = [&](float x) {
+        u64 m;
+        const int s = kept_side(x, &m);
+        sum += s > 0 ? m : 0;
+        tie_count += s == 0;
+        tie_mass = s == 0 ? m : tie_mass;
+    };
     if (!nothing) {
-        for (int j = begin; j < stop; ++j) {
-            u64 m;
-            const int s = kept_side(x_s[j], &m);
-            if (s > 0) sum += m;
-            else if (s == 0) {
-                ++tie_count;
-                tie_mass = m;
-            }
+        if (cut.bin >= 0) {
+            each_token_from(floor_x, tally);
+        } else {
+            fours([&](float4 x) {
+                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) >= floor_x)) return;
+                tally(x.x);
+                tally(x.y);
+                tally(x.z);
+                tally(x.w);
+            });
         }
     }
-    u64 cta_sum;
-    uint32_t cta_ties;
-    const u64 sum_before = block_exclusive_scan<u64>(sum, scan64_s, &cta_sum);
-    const uint32_t ties_before = block_exclusive_scan<uint32_t>(tie_count, scan32_s, &cta_ties);
-    if (tid == 0) {
-        total_mass_s = cta_sum;
-        total_ties_s = cta_ties;
-        tie_mass_s = 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        tie_count += __shfl_xor_sync(0xffffffffu, tie_count, o);
+        tie_mass = max(tie_mass, __shfl_xor_sync(0xffffffffu, tie_mass, o));
+    }
+    if (lane == 0) {
+        run_sum_s[tid >> 5] = sum;
+        run_ties_s[tid >> 5] = tie_count;
+        run_tie_mass_s[tid >> 5] = tie_mass;
     }
     __syncthreads();
-    if (tie_count) tie_mass_s = tie_mass;                                          // (the same from every thread)
+    if (tid < 32) {                                                                // what lies before each run; the CTA's totals
+        u64 m = lane < threads / 32 ? run_sum_s[lane] : 0, before = m;
+        uint32_t c = lane < threads / 32 ? run_ties_s[lane] : 0, ties_before = c;
+        u64 one = lane < threads / 32 ? run_tie_mass_s[lane] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 y = __shfl_up_sync(0xffffffffu, before, o);
+            const uint32_t z = __shfl_up_sync(0xffffffffu, ties_before, o);
+            if (lane >= o) {
+                before += y;
+                ties_before += z;
+            }
+            one = max(one, __shfl_xor_sync(0xffffffffu, one, o));
+        }
+        run_sum_s[lane] = before - m;
+        run_ties_s[lane] = ties_before - c;
+        if (lane == 31) {
+            total_mass_s = before;
+            total_ties_s = ties_before;
+            tie_mass_s = one;
+            run_found_s = -1;
+        }
+    }
     sync();
     u64 total = 0, cta_before = 0;
     uint32_t all_ties = 0, cta_ties_before = 0;
     tie_mass = 0;
-    for (int c = 0; c < ctas; ++c) {
+#pragma unroll
+    for (int c = 0; c < MAX_CLUSTER; ++c) {
         if (c == rank) {
             cta_before = total;
             cta_ties_before = all_ties;
         }
-        total += *cluster.map_shared_rank(&total_mass_s, c);
-        all_ties += *cluster.map_shared_rank(&total_ties_s, c);
-        tie_mass = max(tie_mass, *cluster.map_shared_rank(&tie_mass_s, c));
+        if (c < ctas) {
+            total += *cluster.map_shared_rank(&total_mass_s, c);
+            all_ties += *cluster.map_shared_rank(&total_ties_s, c);
+            tie_mass = max(tie_mass, *cluster.map_shared_rank(&tie_mass_s, c));
+        }
     }
     auto running = [&](u64 m, uint32_t t) { return m + min(t, ties) * tie_mass; };
     const u64 whole = running(total, all_ties);
@@ -401,40 +625,36 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         const float u = a.uniforms[row];
         const double wanted = floor((u > 0.f ? fmin((double)u, 1.0) : 0.0) * (double)whole);
         const u64 target = min((u64)wanted, whole - 1);
-        u64 m0 = cta_before + sum_before;
-        uint32_t t0 = cta_ties_before + ties_before;
-        const uint32_t here = __ballot_sync(0xffffffffu, running(m0, t0) <= target && target < running(m0 + sum, t0 + tie_count));
-        if (here) {                                                                // the warp goes through the one thread's tokens
-            const int lane = tid & 31, owner = __ffs(here) - 1;
-            m0 = __shfl_sync(0xffffffffu, m0, owner);
-            t0 = __shfl_sync(0xffffffffu, t0, owner);
-            const int first = __shfl_sync(0xffffffffu, begin, owner), last = __shfl_sync(0xffffffffu, stop, owner);
-            for (int j0 = first; j0 < last; j0 += 32) {
-                const int j = j0 + lane;
-                u64 m = 0;
-                const int s = j < last ? kept_side(x_s[j], &m) : -1;
-                u64 run = s > 0 ? m : 0;
-                uint32_t count = s == 0;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 y = __shfl_up_sync(0xffffffffu, run, o);
-                    const uint32_t c = __shfl_up_sync(0xffffffffu, count, o);
-                    if (lane >= o) {
-                        run += y;
-                        count += c;
-                    }
-                }
-                const uint32_t past = __ballot_sync(0xffffffffu, target < running(m0 + run, t0 + count));
-                if (past) {
-                    if (lane == __ffs(past) - 1) {
+        const u64 m0 = cta_before + run_sum_s[tid >> 5], m1 = cta_before + ((tid >> 5) + 1 < threads / 32 ? run_sum_s[(tid >> 5) + 1] : total_mass_s);
+        const uint32_t t0 = cta_ties_before + run_ties_s[tid >> 5], t1 = cta_ties_before + ((tid >> 5) + 1 < threads / 32 ? run_ties_s[(tid >> 5) + 1] : total_ties_s);
+        if (lane == 0 && running(m0, t0) <= target && target < running(m1, t1)) run_found_s = tid >> 5;
+        __syncthreads();
+        const int run = run_found_s;
+        if (run >= 0) {                                                            // (the whole CTA: a few neighbours per thread)
+            const int per = (run4 * 4 + threads - 1) / threads, begin = run * run4 * 4 + tid * per, stop = min(n, min(begin + per, (run + 1) * run4 * 4));
+            u64 mine = 0, all;
+            uint32_t my_ties = 0, all_run_ties;
+            for (int j = begin; j < stop; ++j) {
+                u64 m;
+                const int s = kept_side(x_s[j], &m);
+                mine += s > 0 ? m : 0;
+                my_ties += s == 0;
+            }
+            u64 at = cta_before + run_sum_s[run] + block_exclusive_scan<u64>(mine, scan64_s, &all);
+            uint32_t tie_at = cta_ties_before + run_ties_s[run] + block_exclusive_scan<uint32_t>(my_ties, scan32_s, &all_run_ties);
+            if (running(at, tie_at) <= target && target < running(at + mine, tie_at + my_ties)) {
+                for (int j = begin; j < stop; ++j) {
+                    u64 m;
+                    const int s = kept_side(x_s[j], &m);
+                    at += s > 0 ? m : 0;
+                    tie_at += s == 0;
+                    if (target < running(at, tie_at)) {
                         a.tokens[row] = (int32_t)((long long)unit0 * VE + j - skip);
                         if (a.logprobs)
                             a.logprobs[row] = r.greedy ? 0.f : (float)((x_s[j] == r.largest ? 0.0 : ((double)x_s[j] - (double)r.largest) * inverse_t) - log((double)whole / unit));
+                        break;
                     }
-                    break;
                 }
-                m0 += __shfl_sync(0xffffffffu, run, 31);
-                t0 += __shfl_sync(0xffffffffu, count, 31);
             }
         }
     }
