@@ -7,12 +7,13 @@
 //
 // A row lies in the shared memory of one cluster of 1 to 8 CTAs, read from memory once.  Masses are integers, w in units of 2^-F with F = 62 -
 // ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included.  w = 2^(n / 256 + f / 256) in 64 bits, |f| <= 1 / 2:
-// 2^(n mod 256 / 256) from a table, the rest by its series to the third power (Tang 1989; relative error 2e-13): a third of the instructions of exp().
-//   top-k   tokens counted by bins of their distance from the largest (1024 bins); the bin in which the count passes k is cut
-//           into 1024 bins of the values' bit patterns, and so on until a bin holds one token or one value
-//   top-p   the same counts times the bins' weights say near which bin the mass reaches top_p times that of the top-k tokens; the exact mass before
-//           that bin and in it and its neighbours (sums in registers; a bisection if it was none of them) says which, and the bin is cut by masses as above.
-//           (Exact masses per bin from the start are two more atomics per token, which return: 64 rows of 100 003 logits 81 us against MEASURED.)
+// 2^(n mod 256 / 256) from a table, the rest by its series to the third power (Tang 1989; relative error 2e-13).  (64 rows of 100 003 logits without
+// filters: exp() 40 us over a pass that only looks for the largest, this 10.5, the same on sums of two fp32 numbers, 36 instructions, 21, with the
+// conversions from and to 64 bits done on the bits 14.)
+//   top-k   tokens counted by bins of their distance from the largest (896 of them); the bin in which the count passes k is cut
+//           into 512 bins of the values' bit patterns, and so on until a bin holds one token or one value
+//   top-p   the same descent on the bins' masses, from the same first histogram, towards top_p times the mass of the top-k tokens.  (Counts alone in the
+//           first histogram, the masses around a guessed bin by a pass of their own: 86 us against MEASURED for 64 rows of 100 003.)
 // A histogram is reduced by the cluster (a CTA sums a share of the bins over all CTAs and hands the sums to all), two cluster barriers.
 // What bounds it: launches of a few rows the chain of barriers, many rows the exponentials' and the histogram's instructions.
 #include <cooperative_groups.h>
@@ -31,7 +32,7 @@ namespace {
 namespace cg = cooperative_groups;
 using u64 = unsigned long long;
 
-constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 1024, FINE = 512, MAX_SLICE = 51712, MAX_CLUSTER = 8, WINDOW = 16, MAX_VOCAB = 360000;
+constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 896, FINE = 512, MAX_SLICE = 50048, MAX_CLUSTER = 8, MAX_VOCAB = 360000;
 constexpr float BINS_PER_UNIT = 32.f;            // first histogram: bins of 1 / 32 up to 32 below the largest, the rest in the last one
 
 struct SampleArgs {
@@ -45,18 +46,12 @@ struct SampleArgs {
     int32_t histograms;                          // shared memory has room for them
 };
 
-// The first histogram has BINS bins and counts, finer ones FINE bins and masses too.  (As small as this so that two CTAs hold 103 000 fp32
-// logits: by four 64 rows are two waves.)
+// The first histogram has BINS bins, finer ones FINE.  (As small as this so that two CTAs hold 100 000 fp32 logits: by four 64 rows are
+// two waves, 86 us instead of 54.)
 struct Histograms {
-    uint32_t count[BINS], low[FINE], high[FINE];      // this CTA's; a mass's two halves
-    uint32_t all_count[BINS];                         // the cluster's first one
-    union {
-        struct {
-            u64 mass[FINE];
-            uint32_t count[FINE];
-        } fine;                                       // the cluster's finer one
-        float queue[MAX_THREADS / 32][64];            // of each_token_from, before the others may write `fine`
-    };
+    uint32_t count[BINS], low[BINS], high[BINS];      // this CTA's; a mass's two halves
+    u64 all_mass[BINS], fine_mass[FINE];              // the cluster's, of the first and of a finer one
+    uint32_t all_count[BINS], fine_count[FINE];
 };
 
 // What every CTA of a row knows.
@@ -142,7 +137,6 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     __shared__ int run_found_s;
     __shared__ int found_bin_s;
     __shared__ u64 found_mass_s, found_before_s;
-    __shared__ float scanf_s[MAX_THREADS / 32];
     __shared__ u64 part_s[MAX_THREADS / 32][4], cta_part_s[2][4], row_part_s[4];
     __shared__ uint32_t found_count_s;
     const cg::cluster_group cluster = cg::this_cluster();
@@ -220,7 +214,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     Row r;
     r.largest = -INFINITY;
     for (int c = 0; c < ctas; ++c) r.largest = fmaxf(r.largest, *cluster.map_shared_rank(&largest_s, c));
-    const float t = a.temperature ? a.temperature[row] : 1.f;
+    const float t = a.temperature ? a.temperature[row] : 1.f, u = a.uniforms[row];
     r.greedy = !(t > 0.f);
     const double inverse_t = 1.0 / (double)t;
     r.places = a.places;
@@ -236,25 +230,9 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     const bool nothing = r.largest == -INFINITY;
 
     // ---- a histogram of the slice's tokens, summed over the cluster into all_*[which] ----
-    auto reduce_first = [&] {
+    auto reduce = [&](bool fine, bool masses) {
         sync();
-        const int share = BINS / ctas;
-        for (int b = tid; b < share; b += threads) {
-            const int at = rank * share + b;
-            uint32_t count[MAX_CLUSTER], all = 0;
-#pragma unroll
-            for (int c = 0; c < MAX_CLUSTER; ++c) count[c] = c < ctas ? cluster.map_shared_rank(hist, c)->count[at] : 0;
-#pragma unroll
-            for (int c = 0; c < MAX_CLUSTER; ++c) all += count[c];
-#pragma unroll
-            for (int c = 0; c < MAX_CLUSTER; ++c)
-                if (c < ctas) cluster.map_shared_rank(hist, c)->all_count[at] = all;
-        }
-        sync();
-    };
-    auto reduce_fine = [&](bool masses) {
-        sync();
-        const int share = FINE / ctas;
+        const int share = (fine ? FINE : BINS) / ctas;
         for (int b = tid; b < share; b += threads) {
             const int at = rank * share + b;
             uint32_t count[MAX_CLUSTER], low[MAX_CLUSTER], high[MAX_CLUSTER];
@@ -281,15 +259,15 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             for (int c = 0; c < MAX_CLUSTER; ++c)
                 if (c < ctas) {
                     Histograms* h = cluster.map_shared_rank(hist, c);
-                    h->fine.count[at] = all;
-                    h->fine.mass[at] = m;
+                    (fine ? h->fine_count : h->all_count)[at] = all;
+                    (fine ? h->fine_mass : h->all_mass)[at] = m;
                 }
         }
         sync();
     };
+    static_assert(BINS % MAX_CLUSTER == 0 && FINE % MAX_CLUSTER == 0, "shares");
     auto clear = [&] {
-        for (int b = tid; b < BINS; b += threads) hist->count[b] = 0;
-        for (int b = tid; b < FINE; b += threads) hist->low[b] = hist->high[b] = 0;
+        for (int b = tid; b < BINS; b += threads) hist->count[b] = hist->low[b] = hist->high[b] = 0;
         __syncthreads();
     };
     auto add = [&](int b, u64 m) {
@@ -302,18 +280,22 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     // The bin (of the first or a finer histogram) in which the count passes `want` (by_mass: the mass reaches `target`), and what of either lies
     // before it.
     auto find = [&](bool fine, bool by_mass, uint32_t want, double target, u64 base0) {
-        const int bins = fine ? FINE : BINS, per = max(1, bins / threads), at = tid * per;
-        auto count_of = [&](int b) { return fine ? hist->fine.count[b] : hist->all_count[b]; };
-        u64 sum = 0, all;
-        for (int b = at; b < min(bins, at + per); ++b) sum += by_mass ? hist->fine.mass[b] : count_of(b);
-        u64 before = base0 + block_exclusive_scan<u64>(sum, scan64_s, &all);
+        const int bins = fine ? FINE : BINS, per = (bins + threads - 1) / threads, at = tid * per;
+        const uint32_t* counts = fine ? hist->fine_count : hist->all_count;
+        const u64* masses = fine ? hist->fine_mass : hist->all_mass;
+        u64 count = 0, m = 0, all;
         for (int b = at; b < min(bins, at + per); ++b) {
-            const u64 step = by_mass ? hist->fine.mass[b] : count_of(b);
+            count += counts[b];
+            m += masses[b];
+        }
+        u64 before = base0 + block_exclusive_scan<u64>(by_mass ? m : count, scan64_s, &all);
+        for (int b = at; b < min(bins, at + per); ++b) {
+            const u64 step = by_mass ? masses[b] : counts[b];
             const bool here = by_mass ? (double)before < target && (double)(before + step) >= target : before < want && before + step >= want;
             if (here) {
                 found_bin_s = b;
-                found_count_s = count_of(b);
-                found_mass_s = fine ? hist->fine.mass[b] : 0;
+                found_count_s = counts[b];
+                found_mass_s = masses[b];
                 found_before_s = before;
             }
             before += step;
@@ -336,27 +318,15 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             f(x.w);
         }
     };
-    // The tokens from `from` up, in whole warps: what costs tens of instructions per token is not done for those below.
-    float* queue = hist->queue[tid >> 5];
+    // ... but for those all of whose neighbours in the warp are below `from`
     auto each_token_from = [&](float from, auto f) {
-        int count = 0;
-        fours([&](float4 x4) {
-            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t mask = __ballot_sync(0xffffffffu, x[e] >= from);
-                if (x[e] >= from) queue[count + __popc(mask & ((1u << lane) - 1))] = x[e];
-                count += __popc(mask);
-                if (count >= 32) {
-                    __syncwarp();
-                    count -= 32;
-                    f(queue[count + lane]);
-                    __syncwarp();
-                }
-            }
+        fours([&](float4 x) {
+            if (!__any_sync(0xffffffffu, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) >= from)) return;
+            f(x.x);
+            f(x.y);
+            f(x.z);
+            f(x.w);
         });
-        __syncwarp();
-        if (count > 0) f(lane < count ? queue[lane] : -INFINITY);
     };
     // Four sums over the threads of the whole cluster, in row_part_s
     int flip = 0;
@@ -396,15 +366,15 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             clear();
             fours([&](float4 x4) {
                 const float x[4] = {x4.x, x4.y, x4.z, x4.w};
-                if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) < c.from) return;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    const bool near = x[e] >= c.from && x[e] <= c.to;
+                    if (!__any_sync(0xffffffffu, near)) continue;
                     const uint32_t key = key_of<T>(x[e]);
-                    if (x[e] >= c.from && x[e] <= c.to && key - c.low <= range && first_bin(r, x[e]) == c.bin)
-                        add((int)((c.high - key) >> shift), by_mass ? mass(r, table_s, x[e]) : 0);
+                    if (near && key - c.low <= range && first_bin(r, x[e]) == c.bin) add((int)((c.high - key) >> shift), by_mass ? mass(r, table_s, x[e]) : 0);
                 }
             });
-            reduce_fine(by_mass);
+            reduce(true, by_mass);
             find(true, by_mass, want, target, before);
             const uint32_t top = c.high - ((uint32_t)found_bin_s << shift), span = (1u << shift) - 1;
             c.low = top - c.low > span ? top - span : c.low;
@@ -432,97 +402,50 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     Cut cut{-1, 0.f, 0.f, 0u, 0u, 0u};
     if (!nothing && !r.greedy && (use_k || use_p)) {
         clear();
-        u64 s0 = 0, s1 = 0;
-        uint32_t s2 = 0;
-        if (use_k) each_token([&](float x) { atomicAdd(&hist->count[first_bin(r, x)], 1u); });
-        else each_token([&](float x) {
-            atomicAdd(&hist->count[first_bin(r, x)], 1u);
-            s0 += mass(r, table_s, x);
-        });
-        reduce_first();
-        if (use_k) {
-            find(false, false, (uint32_t)k, 0.0, 0);
+        if (use_p) each_token([&](float x) { add(first_bin(r, x), mass(r, table_s, x)); });
+        else each_token([&](float x) { atomicAdd(&hist->count[first_bin(r, x)], 1u); });
+        reduce(false, use_p);
+        u64 kept;
+        auto found = [&](bool by_mass, uint32_t want, double target) {
             const int bin = found_bin_s;
             const uint32_t count = found_count_s;
-            const u64 before = found_before_s;
+            const u64 before = found_before_s, m = found_mass_s;
             __syncthreads();
-            cut = descend(bin, count, false, (uint32_t)k, 0.0, before, 0);
+            return descend(bin, count, by_mass, want, target, before, m);
+        };
+        if (use_k) {
+            find(false, false, (uint32_t)k, 0.0, 0);
+            cut = found(false, (uint32_t)k, 0.0);
         }
         if (use_p) {
-            if (use_k)                                                             // masses above the cut and at it, tokens at it
-                each_token_from(cut.from, [&](float x) {
-                    const int s = side<T>(r, cut, x);
-                    const u64 m = s >= 0 ? mass(r, table_s, x) : 0;
-                    s0 += s > 0 ? m : 0;
-                    s1 += s == 0 ? m : 0;
-                    s2 += s == 0;
-                });
-            sum_over_row(s0, s1, s2, 0);
-            const u64 kept = row_part_s[0] + (row_part_s[2] ? row_part_s[1] / row_part_s[2] * cut.ties : 0);
-            const double target = fmax((double)top_p * (double)kept, 0.5);         // (the largest is always kept)
-            // near which bin: counts times the weights in the bins' middles, in proportion to a mass that is known (values that sit at one edge
-            // of their bins, as bf16 ones do, weigh a per cent more than that: a dozen bins)
-            const int per = BINS / threads, at = tid * per;
-            const float bin_scale = (float)(-r.scale / (256.0 * BINS_PER_UNIT));
-            auto guess = [&](int b) { return (float)hist->all_count[b] * exp2f((b + 0.5f) * bin_scale); };
-            float sum = 0.f, all;
-            for (int b = 0; b < per; ++b)
-                if (!use_k || at + b <= cut.bin) sum += guess(at + b);
-            const float guess_before = block_exclusive_scan<float>(sum, scanf_s, &all);
-            auto guess_bin = [&](float near) {                                     // the bin in which the guesses' sum passes `near`, -1: none
-                if (tid == 0) found_bin_s = -1;
-                __syncthreads();
-                float reached = guess_before;
-                for (int b = 0; b < per; ++b) {
-                    const float to = reached + guess(at + b);
-                    if (reached < near && to >= near) found_bin_s = at + b;
-                    reached = to;
-                }
-                __syncthreads();
-                const int bin = found_bin_s;
-                __syncthreads();
-                return bin;
-            };
-            int bin = guess_bin((float)(target / (double)max(kept, 1ull)) * all), lo = 0, hi = BINS - 1;      // the one that reaches the target lies in [lo, hi]
-            for (;;) {
-                // the exact mass before a window of bins around the guess, and in each of them
-                if (bin < lo || bin > hi) bin = (lo + hi) / 2;
-                const int b0 = max(lo, min(bin - WINDOW / 2, hi - (WINDOW - 1)));
-                u64 above = 0, inside = 0;
-                clear();
-                each_token_from(bin_from(r, b0 + WINDOW - 1), [&](float x) {
-                    const int b = first_bin(r, x) - b0;
-                    const u64 m = mass(r, table_s, x);
-                    above += b < 0 ? m : 0;
-                    if (b >= 0 && b < WINDOW && x > -INFINITY) {
-                        inside += m;
-                        add(b, m);
+            u64 part = 0, tie = 0;                                                 // the mass of what is kept so far
+            uint32_t tie_tokens = 0;
+            for (int b = tid; b < BINS; b += threads)
+                if (!use_k || b < cut.bin) part += hist->all_mass[b];
+            if (use_k) {
+                part = rank == 0 ? part : 0;
+                fours([&](float4 x4) {
+                    const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool near = x[e] >= cut.from && x[e] <= cut.to;
+                        if (!__any_sync(0xffffffffu, near)) continue;
+                        const int s = near && first_bin(r, x[e]) == cut.bin ? side<T>(r, cut, x[e]) : -1;
+                        const u64 m = mass(r, table_s, x[e]);
+                        part += s > 0 ? m : 0;
+                        tie += s == 0 ? m : 0;
+                        tie_tokens += s == 0;
                     }
                 });
-                sum_over_row(above, inside, 0, 0);
-                const u64 before = row_part_s[0];
-                if ((double)before < target && (double)(before + row_part_s[1]) >= target) {
-                    reduce_fine(true);
-                    find(true, true, 0u, target, before);
-                    bin = b0 + found_bin_s;
-                    const uint32_t count = found_count_s;
-                    const u64 before_bin = found_before_s, m = found_mass_s;
-                    __syncthreads();
-                    cut = descend(bin, count, true, 0u, target, before_bin, m);
-                    break;
-                }
-                if ((double)before >= target) hi = b0 - 1;
-                else lo = b0 + WINDOW;
-                if (b0 >= at && b0 < at + per) {                                   // again, in proportion to the mass before b0
-                    float reached = guess_before;
-                    for (int b = at; b < b0; ++b) reached += guess(b);
-                    scanf_s[0] = reached;
-                }
+                sum_over_row(part, tie, tie_tokens, 0);
+                kept = row_part_s[0] + (row_part_s[2] ? row_part_s[1] / row_part_s[2] * cut.ties : 0);
+            } else {
+                block_exclusive_scan<u64>(part, scan64_s, &kept);
                 __syncthreads();
-                const float reached = scanf_s[0];
-                __syncthreads();
-                bin = guess_bin((float)(target / (double)max(before, 1ull)) * reached);
             }
+            const double target = fmax((double)top_p * (double)kept, 0.5);         // (the largest is always kept)
+            find(false, true, 0u, target, 0);
+            cut = found(true, 0u, target);
         }
     }
 
@@ -551,17 +474,25 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         tie_mass = s == 0 ? m : tie_mass;
     };
     if (!nothing) {
-        if (cut.bin >= 0) {
-            each_token_from(floor_x, tally);
-        } else {
-            fours([&](float4 x) {
-                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) >= floor_x)) return;
-                tally(x.x);
-                tally(x.y);
-                tally(x.z);
-                tally(x.w);
+        if (cut.bin < 0 && !r.greedy)
+            each_token_from(floor_x, [&](float x) {
+                const u64 m = mass(r, table_s, x);
+                sum += m >= least ? m : 0;
             });
-        }
+        else if (r.greedy)
+            each_token_from(floor_x, tally);
+        else
+            fours([&](float4 x4) {
+                const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= floor_x)) return;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const u64 m = mass(r, table_s, x[e]);
+                    sum += x[e] > cut.to && m >= least ? m : 0;                    // above the cut's bin
+                    const bool near = x[e] >= cut.from && x[e] <= cut.to;
+                    if (__any_sync(0xffffffffu, near) && near) tally(x[e]);
+                }
+            });
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -622,7 +553,6 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             if (a.logprobs) a.logprobs[row] = -INFINITY;
         }
     } else {
-        const float u = a.uniforms[row];
         const double wanted = floor((u > 0.f ? fmin((double)u, 1.0) : 0.0) * (double)whole);
         const u64 target = min((u64)wanted, whole - 1);
         const u64 m0 = cta_before + run_sum_s[tid >> 5], m1 = cta_before + ((tid >> 5) + 1 < threads / 32 ? run_sum_s[(tid >> 5) + 1] : total_mass_s);
