@@ -12,7 +12,7 @@
 // binds), and the memory of their tiles, where the queries find room.
 //
 // One CTA = (128 rows of the state, value head, sequence), all chunks of the sequence in order.  The state's rows lie in registers, a row in
-// two threads (a half each), which are in the two CHAIN warpgroups; all products have the rows as M = 128 lanes:
+// two threads (a half each; dk = 64: four), one in each CHAIN warpgroup; all products have the rows as M = 128 lanes:
 //      S [K; Q]^T       one MMA set for Z and S Q^T (N = 128; the low half of S for Z alone where outputs are bf16)
 //      X T^T, D K, D P^T
 // PREPARING warpgroups take the chunks in turn: keys and queries to an operand tile (128 rows: 64 of K, 64 of Q), [K; Q] K^T in one MMA set,
@@ -60,7 +60,7 @@ struct Shape {
     static constexpr int PARTS = WIDE_T ? 2 : 1;                   // fp16 parts of a key, a query, P
     static constexpr int PREPS = WIDE_T && D == 128 ? 1 : 2;       // preparing teams
     static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = 2;
-    static constexpr int PREP_THREADS = 128 * PREPS, CHAIN_THREADS = 256, THREADS = PREP_THREADS + CHAIN_THREADS + 128;
+    static constexpr int PREP_THREADS = 128 * PREPS, GROUPS = D == 64 ? 4 : 2, CHAIN_THREADS = 128 * GROUPS, THREADS = PREP_THREADS + CHAIN_THREADS + 128;
     static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK, T_BYTES = 2 * TILE, P_BYTES = PARTS * TILE;
     static constexpr bool STAGE_V = !WIDE_T;                       // values through shared memory (fp32: there is no room)
     static constexpr int V_BYTES = STAGE_V ? C * ROWS * (int)sizeof(T) : 0;
@@ -68,14 +68,14 @@ struct Shape {
     // per K stage: beta g / key scale, g / query scale, beta, g_C; per T stage: weights of D's columns for the state, what undoes P's rows' scales
     // and T's
     static constexpr int KCO = 3 * C + 4, TCO = 2 * C + 4;
-    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + 12 * ROWS) * 4 + 256;
+    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + (2 * GROUPS + 4) * ROWS) * 4 + 256;
     static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
     static_assert(SMEM <= 232448, "shared memory");
     // tensor memory: S operand / D K | Z, X operand, D operand for the outputs (64) ; S Q^T (64) | D (64) | D P^T (64) | per preparing team 64
     static constexpr uint32_t Z_COL = 128, O1_COL = Z_COL + C, D_COL = 256, O2_COL = 320, PREP_COL = 384, TMEM_COLS = 512;
-    // registers: 640 threads start with 96 each; the roles share them as they need them
-    static constexpr bool SPLIT_REGS = THREADS == 640;
-    static constexpr int PREP_REGS = D == 128 ? 72 : 88, CHAIN_REGS = D == 128 ? 128 : 112, OUT_REGS = 80;
+    // registers: 640 threads start with 96 each; at dk = 128 the chain's state rows take what the other roles leave
+    static constexpr bool SPLIT_REGS = THREADS == 640 && D == 128;
+    static constexpr int PREP_REGS = 72, CHAIN_REGS = 128, OUT_REGS = 80;
     static_assert(!SPLIT_REGS || 2 * PREP_REGS + 2 * CHAIN_REGS + OUT_REGS <= 5 * 96, "a split beyond the launch's registers waits for ever");
 };
 
@@ -104,8 +104,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
     float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);
     float* tco_s = kco_s + Z::K_STAGES * Z::KCO;
     float* tok_s = tco_s + Z::T_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
-    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [4][2][ROWS] largest of a half row: S, X, D, D as weighted
-    float* inv_s = max_s + 8 * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
+    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [2][GROUPS][ROWS] largest of a row's part: S, X, D in turn; D as weighted
+    float* inv_s = max_s + 2 * Z::GROUPS * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
     uint64_t* bars = reinterpret_cast<uint64_t*>(inv_s + 4 * ROWS);
     auto bar_k = [&](int i) { return smem_u32(bars + i % Z::K_STAGES); };           // keys, queries, their weights
     auto bar_kfree = [&](int i) { return smem_u32(bars + 3 + i % Z::K_STAGES); };
@@ -467,20 +467,27 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             proxy_fence();
             arrive(bar_t(i));
         }
-    } else if (warp < 4 * Z::PREPS + 8) {
+    } else if (warp < 4 * (Z::PREPS + Z::GROUPS)) {
         // =============================== STATE ROWS ===============================
         if constexpr (Z::SPLIT_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Z::CHAIN_REGS));
-        constexpr int H = D / 2, HB = H / 16;                     // a thread's part of its row, in blocks of 16
+        constexpr int G = Z::GROUPS, H = D / G, HB = H / 16, TG = C / G, TB = TG / 16;      // a thread's part of its row and of the tokens, in blocks of 16
         const int c = (warp >> 2) - Z::PREPS, r = (warp & 3) * 32 + lane;
         const bool is_row = row_base + r < a.dv;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem_base + lanes + c * H, z_at = tmem_base + lanes + Z::Z_COL + 32 * c, d_at = tmem_base + lanes + Z::D_COL + 32 * c;
+        const uint32_t s_at = tmem_base + lanes + c * H, z_at = tmem_base + lanes + Z::Z_COL + TG * c, d_at = tmem_base + lanes + Z::D_COL + TG * c;
         const bool issuer = warp == 4 * Z::PREPS, leader = issuer && lane == 0;
-        float* mine = max_s + c * ROWS + r;                       // + 2 ROWS per kind
-        const float* other = max_s + (1 - c) * ROWS + r;
+        // largest magnitudes (kind 0: S, X, D in turn, barriers between them; 1: D as weighted): mine, and of the whole row when all have met
+        float* mine = max_s + c * ROWS + r;
+        auto of_row = [&](int kind) {
+            const float* m = max_s + kind * G * ROWS + r;
+            float x = fmaxf(m[0], m[ROWS]);
+#pragma unroll
+            for (int e = 2; e < G; ++e) x = fmaxf(x, m[e * ROWS]);
+            return x;
+        };
         float* state = a.states + seq.slot * a.state_stride + ((long long)hv * a.dv + row_base + r) * D + c * H;
         auto meet = [&] { return bar_or(CHAIN_BARRIER, Z::CHAIN_THREADS, fail ? 1 : 0); };
-        // the row's half, times 2^e; inv_row, scale_row: 2^-e, 2^e.  The exponent changes only when the row's largest element leaves a
+        // the row's part, times 2^e; inv_row, scale_row: 2^-e, 2^e.  The exponent changes only when the row's largest element leaves a
         // window in which two fp16 parts hold it to 22 bits.
         float S[H], m = 0.f, inv_row = 1.f, scale_row = 1.f;
 #pragma unroll
@@ -500,7 +507,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             const float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
             float sc;
             // ---- Z = S K^T, and S Q^T ----
-            m = fmaxf(m, *other);
+            m = of_row(0);
             if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f)) {
                 float inv;
                 pow2_scale(m, WIDE, sc, inv);
@@ -544,36 +551,36 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 }
                 mma_commit(bar_z);
             }
-            float val[Z::STAGE_V ? 1 : 32];                       // fp32 values: from global memory, beside the product
+            float val[Z::STAGE_V ? 1 : TG];                       // fp32 values: from global memory, beside the product
             if constexpr (Z::STAGE_V) {
                 wait(bar_v, turn);
             } else {
                 const T* vp = static_cast<const T*>(a.v) + seq.begin * a.v_stride + (long long)hv * a.dv + row_base + r;
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int t = i * C + 32 * c + e;
+                for (int e = 0; e < TG; ++e) {
+                    const int t = i * C + TG * c + e;
                     val[e] = is_row && t < seq.length ? __ldg(reinterpret_cast<const float*>(vp + t * a.v_stride)) : 0.f;
                 }
             }
             wait_mma(bar_z, turn);
             tc_fence_after();
             // ---- X = (V^T - Z diag(g)) diag(beta) ----
-            float x[32], mx = 0.f;
+            float x[TG], mx = 0.f;
             const float2 neg = pair(-inv_row, -inv_row);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < TB; ++b) {
                 uint32_t v[16];
                 tmem_ld16(z_at + 16 * b, v);
                 float u[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    if constexpr (Z::STAGE_V) u[e] = __bfloat162float(v_s[(32 * c + 16 * b + e) * ROWS + r]);
+                    if constexpr (Z::STAGE_V) u[e] = __bfloat162float(v_s[(TG * c + 16 * b + e) * ROWS + r]);
                     else u[e] = val[16 * b + e];
                 }
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    const float4 gz = *reinterpret_cast<const float4*>(kco + 32 * c + 16 * b + e), be = *reinterpret_cast<const float4*>(kco + 2 * C + 32 * c + 16 * b + e);
+                    const float4 gz = *reinterpret_cast<const float4*>(kco + TG * c + 16 * b + e), be = *reinterpret_cast<const float4*>(kco + 2 * C + TG * c + 16 * b + e);
                     const float2 y0 = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), neg), pair(gz.x, gz.y), __fmul2_rn(pair(u[e], u[e + 1]), pair(be.x, be.y)));
                     const float2 y1 = __ffma2_rn(__fmul2_rn(pair(v[e + 2], v[e + 3]), neg), pair(gz.z, gz.w), __fmul2_rn(pair(u[e + 2], u[e + 3]), pair(be.z, be.w)));
                     x[16 * b + e] = y0.x; x[16 * b + e + 1] = y0.y; x[16 * b + e + 2] = y1.x; x[16 * b + e + 3] = y1.y;
@@ -581,13 +588,13 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 }
             }
             const float g_chunk = kco[3 * C];
-            mine[2 * ROWS] = mx;
+            *mine = mx;
             if (meet()) { fail = true; break; }
             if (Z::STAGE_V && leader) arrive(bar_vfree);
             float inv_x;
-            pow2_scale(fmaxf(mx, other[2 * ROWS]), WIDE, sc, inv_x);
+            pow2_scale(of_row(0), WIDE, sc, inv_x);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
+            for (int b = 0; b < TB; ++b) split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
             tc_wait_st();
             tc_fence_before();
             wait(bar_t(i), t_turn(i));
@@ -608,34 +615,34 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             // ---- D's operands: times g_C / g (and what undoes the keys' scales) for the state, as it is for the outputs ----
             float my = 0.f, me = 0.f;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < TB; ++b) {
                 uint32_t v[16];
                 tmem_ld16(d_at + 16 * b, v);
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
+                    const float4 w = *reinterpret_cast<const float4*>(tco + TG * c + 16 * b + e);
                     const float2 d0 = pair(v[e], v[e + 1]), d1 = pair(v[e + 2], v[e + 3]), e0 = __fmul2_rn(d0, pair(w.x, w.y)), e1 = __fmul2_rn(d1, pair(w.z, w.w));
                     x[16 * b + e] = d0.x; x[16 * b + e + 1] = d0.y; x[16 * b + e + 2] = d1.x; x[16 * b + e + 3] = d1.y;
                     my = max3(max3(my, d0.x, d0.y), d1.x, d1.y);
                     me = max3(max3(me, e0.x, e0.y), e1.x, e1.y);
                 }
             }
-            mine[4 * ROWS] = my;
-            mine[6 * ROWS] = me;
+            *mine = my;
+            mine[G * ROWS] = me;
             const float undo = inv_x * tco[2 * C];
             if (meet()) { fail = true; break; }
             float inv_d, inv_e, sc_e;
-            pow2_scale(fmaxf(my, other[4 * ROWS]), WIDE, sc, inv_d);
-            pow2_scale(fmaxf(me, other[6 * ROWS]), WIDE, sc_e, inv_e);
+            pow2_scale(of_row(0), WIDE, sc, inv_d);
+            pow2_scale(of_row(1), WIDE, sc_e, inv_e);
             if (c == 0) inv_s[(2 + turn) * ROWS + r] = inv_d * undo;
             const float back = (inv_e * undo) * scale_row;            // of D K, to the state rows' units
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < TB; ++b) {
                 float y[16];
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    const float4 w = *reinterpret_cast<const float4*>(tco + 32 * c + 16 * b + e);
+                    const float4 w = *reinterpret_cast<const float4*>(tco + TG * c + 16 * b + e);
                     const float2 e0 = __fmul2_rn(pair(x[16 * b + e], x[16 * b + e + 1]), pair(w.x, w.y)), e1 = __fmul2_rn(pair(x[16 * b + e + 2], x[16 * b + e + 3]), pair(w.z, w.w));
                     y[e] = e0.x; y[e + 1] = e0.y; y[e + 2] = e1.x; y[e + 3] = e1.y;
                 }
