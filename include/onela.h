@@ -312,7 +312,8 @@ onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream)
  * tokens keeps its state (or, fresh, gets the zero state).  Found on the device, with *status_dev, if given, set to {ONELA_E_DEVICE_CHECK, sequence}
  * by one that finds it (the caller clears the words): a slot of num_states or more, or that an earlier sequence of the call has, and row
  * ranges that run backwards, begin before an earlier sequence's or leave [0, n_tokens]; such a sequence is treated as padded.
- * States, outputs and inputs do not overlap.
+ * States, outputs and inputs do not overlap.  In chunks, a token whose q, k, v or gates are not finite can make the outputs of up to 63 tokens before
+ * it not finite too (what follows it is lost either way).
  * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it
  * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores.
  * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED.

@@ -180,7 +180,6 @@ struct onela_ctx {
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // Requests of a batched call must exist and share beam width and depth.
 onela_status check_batch(const onela_ctx* ctx, int32_t req_begin, int32_t req_count) {

@@ -19,7 +19,10 @@ namespace onela {
 namespace {
 
 constexpr int WARPS = 4;
-constexpr int CHUNKED_FROM = 32;          // tokens of the longest sequence from which the chunked kernel is the faster one
+// Tokens of the longest sequence from which the chunked kernel is the faster one.  Measured, us token by token / in chunks: 128 x 128 bf16, 16 heads, one
+// sequence of 24 11.3 / 18.3, 32 14.4 / 18.4, 48 20.6 / 18.4; four of 24 17.3 / 18.6, 32 22.1 / 18.6; 37 of 24 72 / 74, 32 93 / 75; 32 heads, four of 16
+// 20.3 / 19.1; 64 x 64 fp32, 16 heads, one of 32 10.6 / 13.6, 48 15.0 / 13.7, 37 of 32 39.6 / 55, 64 74 / 56.
+constexpr int CHUNKED_FROM = 32;
 
 template <typename T>
 __device__ __forceinline__ void load4(const T* p, float* x);
@@ -178,18 +181,20 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
     if (g->num_sequences > 65535 || g->n_tokens > 0x7fffff00ll) return ONELA_E_CAPACITY;
     if (!g->starts_dev && g->n_tokens != g->num_sequences) return ONELA_E_INVAL;
     if (!g->slots_dev && g->num_states < g->num_sequences) return ONELA_E_INVAL;
-    if (g->num_sequences == 0 || g->num_states == 0) return ONELA_OK;
+    if (g->num_sequences == 0) return ONELA_OK;
     const long long es = g->dtype == ONELA_DTYPE_BF16 ? 2 : 4, big = 1ll << 40;
-    auto rows_ok = [&](const void* p, long long stride, long long extent, long long size) {
-        return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride >= extent && stride < big && stride * size % 16 == 0;
+    auto rows = [](const void* p, long long stride, long long extent, long long size, long long n) {
+        return Rows{static_cast<const char*>(p), stride * size, extent * size, n};
     };
-    if (!rows_ok(g->states_dev, g->state_stride, (long long)g->num_v_heads * g->dv * g->dk, 4)) return ONELA_E_INVAL;
-    if (g->n_tokens > 0) {
-        if (!rows_ok(g->q_dev, g->q_stride, (long long)g->num_heads * g->dk, es) || !rows_ok(g->k_dev, g->k_stride, (long long)g->num_heads * g->dk, es) ||
-            !rows_ok(g->v_dev, g->v_stride, (long long)g->num_v_heads * g->dv, es) || !rows_ok(g->out_dev, g->out_stride, (long long)g->num_v_heads * g->dv, es))
-            return ONELA_E_INVAL;
-        if (!g->alpha_dev || !g->beta_dev || g->gate_stride < g->num_v_heads || g->gate_stride >= big) return ONELA_E_INVAL;
-    }
+    // inputs, outputs, states
+    const Rows set[5] = {rows(g->q_dev, g->q_stride, (long long)g->num_heads * g->dk, es, g->n_tokens), rows(g->k_dev, g->k_stride, (long long)g->num_heads * g->dk, es, g->n_tokens),
+                         rows(g->v_dev, g->v_stride, (long long)g->num_v_heads * g->dv, es, g->n_tokens), rows(g->out_dev, g->out_stride, (long long)g->num_v_heads * g->dv, es, g->n_tokens),
+                         rows(g->states_dev, g->state_stride, (long long)g->num_v_heads * g->dv * g->dk, 4, g->num_states)};
+    for (const Rows& r : set)
+        if (r.n > 0 && (!r.base || !aligned16(r.base) || r.stride < r.extent || r.stride >= big || r.stride % 16 != 0)) return ONELA_E_INVAL;
+    if (g->n_tokens > 0 && (!g->alpha_dev || !g->beta_dev || g->gate_stride < g->num_v_heads || g->gate_stride >= big)) return ONELA_E_INVAL;
+    for (int i = 0; i < 4; ++i)
+        if ((i < 3 && share_bytes(set[i], set[3])) || share_bytes(set[i], set[4])) return ONELA_E_INVAL;
     const DeltaArgs a{g->q_dev, g->k_dev, g->v_dev, g->alpha_dev, g->beta_dev, g->states_dev, g->out_dev, g->starts_dev, g->slots_dev, g->fresh_dev, g->status_dev,
                       g->q_stride, g->k_stride, g->v_stride, g->out_stride, g->gate_stride, g->state_stride, g->n_tokens,
                       g->num_sequences, g->num_states, g->num_heads, g->num_v_heads, g->dv, g->dk};

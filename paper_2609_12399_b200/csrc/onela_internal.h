@@ -236,4 +236,24 @@ int decode_sm_count();
 constexpr int WY_MAX_NODES = 160, WY_MAX_DEEP = 64, WY_MAX_LEVELS = 8;
 cudaError_t launch_decode_wy(const DecodeArgs& a, int32_t out_dtype, cudaStream_t stream);
 
+// ---- arguments of the operators without a context ----
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// Rows [base + i stride, + extent) in bytes, i < n
+struct Rows {
+    const char* base;
+    long long stride, extent, n;
+    long long span() const { return n > 0 ? (n - 1) * stride + extent : 0; }
+};
+// Whether two sets of rows share a byte (sets of different strides: whether their spans do).
+inline bool share_bytes(const Rows& x, const Rows& y) {
+    if (x.extent == 0 || y.extent == 0 || x.n == 0 || y.n == 0) return false;
+    const Rows &a = x.base <= y.base ? x : y, &b = x.base <= y.base ? y : x;
+    const long long off = b.base - a.base;
+    if (off >= a.span()) return false;
+    if (a.stride != b.stride) return true;
+    const long long within = off % a.stride;         // b's first row in a's row of the same number, or of a later one
+    if (within < a.extent && off / a.stride < a.n) return true;
+    return within + b.extent > a.stride && off / a.stride + 1 < a.n;
+}
+
 }  // namespace onela

@@ -230,26 +230,6 @@ cudaError_t launch_t(const NormArgs& a, cudaStream_t stream) {
     return two ? launch_shape<T, 16, 2>(a, stream) : launch_shape<T, 32, 1>(a, stream);
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-// Rows [base + i stride, + extent) in bytes, i < n
-struct Rows {
-    const char* base;
-    long long stride, extent, n;
-    long long span() const { return (n - 1) * stride + extent; }
-};
-// Whether two sets of rows share a byte (sets of different strides: whether their spans do).
-bool share_bytes(const Rows& x, const Rows& y) {
-    if (x.extent == 0 || y.extent == 0) return false;
-    const Rows &a = x.base <= y.base ? x : y, &b = x.base <= y.base ? y : x;
-    const long long off = b.base - a.base;
-    if (off >= a.span()) return false;
-    if (a.stride != b.stride) return true;
-    const long long within = off % a.stride;         // b's first row in a's row of the same number, or of a later one
-    if (within < a.extent && off / a.stride < a.n) return true;
-    return within + b.extent > a.stride && off / a.stride + 1 < a.n;
-}
-
 }  // namespace
 }  // namespace onela
 

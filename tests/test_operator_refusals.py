@@ -56,7 +56,10 @@ def test_norm_rotate(lib, kw, status):
     (dict(dk=512), binding.E_UNSUPPORTED), (dict(dv=48), binding.E_UNSUPPORTED), (dict(dv=544), binding.E_UNSUPPORTED), (dict(dv=0), binding.E_UNSUPPORTED),
     (dict(dtype=7), binding.E_INVAL), (dict(n_tokens=-1), binding.E_INVAL), (dict(num_sequences=-1), binding.E_INVAL), (dict(max_tokens=-1), binding.E_INVAL),
     (dict(starts=0), binding.E_INVAL), (dict(slots=0, num_states=2), binding.E_INVAL), (dict(num_sequences=70000), binding.E_CAPACITY),
-    (dict(n_tokens=1 << 31), binding.E_CAPACITY), (dict(num_sequences=0), 0), (dict(num_states=0), 0),
+    (dict(n_tokens=1 << 31), binding.E_CAPACITY), (dict(num_sequences=0), 0),
+    # outputs and states over inputs and over one another
+    (dict(out=A), binding.E_INVAL), (dict(out=3 * A), binding.E_INVAL), (dict(out=2 * A + 256, out_stride=768), binding.E_INVAL), (dict(states=3 * A + 512), binding.E_INVAL),
+    (dict(states=7 * A), binding.E_INVAL),
 ])
 def test_delta_rule(lib, kw, status):
     assert lib.onela_delta_rule(ctypes.byref(_delta(**kw)), None) == status
