@@ -197,10 +197,10 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
         if ((i < 3 && share_bytes(set[i], set[3])) || share_bytes(set[i], set[4])) return ONELA_E_INVAL;
     const DeltaArgs a{g->q_dev, g->k_dev, g->v_dev, g->alpha_dev, g->beta_dev, g->states_dev, g->out_dev, g->starts_dev, g->slots_dev, g->fresh_dev, g->status_dev,
                       g->q_stride, g->k_stride, g->v_stride, g->out_stride, g->gate_stride, g->state_stride, g->n_tokens,
-                      g->num_sequences, g->num_states, g->num_heads, g->num_v_heads, g->dv, g->dk};
+                      g->num_sequences, g->num_states, g->num_heads, g->num_v_heads, g->dv, g->dk, 1};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const long long longest = !g->starts_dev ? 1 : g->max_tokens > 0 ? g->max_tokens : g->n_tokens;
-    const cudaError_t e = longest >= CHUNKED_FROM && delta_chunk_supported(g->dk, g->dv) ? launch_delta_chunk(a, g->dtype, s)
+    const cudaError_t e = longest >= CHUNKED_FROM && delta_chunk_supported(g->dk, g->dv) ? launch_delta_chunk(a, g->dtype, longest, s)
                           : g->dtype == ONELA_DTYPE_BF16 ? launch_step_t<__nv_bfloat16>(a, s) : launch_step_t<float>(a, s);
     return e == cudaSuccess ? ONELA_OK : ONELA_E_CUDA;
 }

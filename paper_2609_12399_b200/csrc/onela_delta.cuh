@@ -14,6 +14,7 @@ struct DeltaArgs {
     int32_t* status;
     long long q_stride, k_stride, v_stride, out_stride, gate_stride, state_stride, n_tokens;
     int32_t num_sequences, num_states, Hk, Hv, dv, dk;
+    int32_t segments;        // pieces that a long sequence is cut into (chunked kernel; 1: none)
 };
 
 // A sequence as the device finds it: where its tokens begin, how many there are, its state.
@@ -62,6 +63,7 @@ __device__ __forceinline__ void report_taken(const DeltaArgs& a, int i) {
 
 // The chunked kernel on the tensor cores (onela_delta_chunk.cu)
 bool delta_chunk_supported(int32_t dk, int32_t dv);
-cudaError_t launch_delta_chunk(const DeltaArgs& a, int32_t dtype, cudaStream_t stream);
+// (longest: tokens that the caller expects of the longest sequence)
+cudaError_t launch_delta_chunk(DeltaArgs a, int32_t dtype, long long longest, cudaStream_t stream);
 
 }  // namespace onela

@@ -19,6 +19,12 @@
 // A's and P's rows from it, T by blocks of 16 and joins, T and P as operand tiles.  An OUTPUT warpgroup brings the values into
 // shared memory and forms and stores O from the two accumulators, beside the chain's next steps.  All of it is coupled by mbarriers over rings.
 //
+// Few long sequences leave most SMs idle, so they are cut into segments (launch_delta_chunk).  The map of a segment is affine, S -> S M + B, and M obeys the
+// recurrence of S from the identity, without values.  Three launches: MAPS, every segment but the last, from zero (B; the first segment from its own
+// state) and, but for the first, from the identity (M), no outputs; FOLD, the segments' states in order (delta_fold_kernel); OUTPUTS, every
+// segment from its state.  The state before a segment, its predecessor's B before that, and M lie meanwhile in the segment's own rows of the caller's `out`, which OUTPUTS overwrites when it
+// has read them: a segment holds enough tokens for that, or its sequence is not cut.
+//
 // Precision.  S, X, D and the results are fp32; operands are sums of two fp16 numbers (22 to 23 significant bits) but for keys and queries
 // in bf16, which one fp16 number holds exactly, and for what only bf16 outputs see (S and D in their products with the queries' side, P): one fp16 number,
 // 2^-12 relative, a sixteenth of the outputs' own rounding.  Every operand row has its own power of two.
@@ -90,7 +96,29 @@ __device__ __forceinline__ float2 pair(uint32_t x, uint32_t y) { return make_flo
 // (the compiler keeps what it knows to be the same in all lanes where the MMAs want it)
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 
-template <int D, typename T>
+enum { WHOLE, MAPS, OUTPUTS };
+
+// The part of a sequence that a CTA works on.
+struct Segment {
+    int p, count;                                 // of how many
+    int begin, length;                            // tokens from the sequence's first, how many
+};
+// Chunks that a segment must have so that its rows of `out` hold B and M, whatever the last chunk holds.
+__host__ __device__ inline int least_chunks(int dk, int dv, int size) { return (int)((((long long)dv + dk) * dk * 4 + (long long)dv * size * C - 1) / ((long long)dv * size * C)) + 1; }
+__device__ __forceinline__ Segment segment_of(int length, int p, int wanted, int dk, int dv, int size) {
+    const int chunks = (length + C - 1) / C;
+    if (wanted < 2 || chunks / wanted < least_chunks(dk, dv, size)) return {p, 1, 0, length};
+    const int first = (int)((long long)chunks * p / wanted), last = (int)((long long)chunks * (p + 1) / wanted);
+    return {p, wanted, first * C, min(length, last * C) - first * C};
+}
+// Float `at` (a multiple of 4) of what lies in the rows of `out` from `row` on, value head hv.
+template <typename T>
+__device__ __forceinline__ float4* scratch(const DeltaArgs& a, long long row, int hv, int at) {
+    const int per = a.dv * (int)sizeof(T) / 4, r = at / per;
+    return reinterpret_cast<float4*>(reinterpret_cast<float*>(static_cast<T*>(a.out) + (row + r) * a.out_stride + (long long)hv * a.dv) + (at - r * per));
+}
+
+template <int D, typename T, int PHASE>
 __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(const DeltaArgs a) {
     using Z = Shape<D, T>;
     constexpr int KB = Z::KB, PARTS = Z::PARTS, KS = (D < 64 ? D : 64) / 16;        // K steps of 16 per block of 64
@@ -124,14 +152,20 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int hv = blockIdx.y, hk = hv / (a.Hv / a.Hk), row_base = blockIdx.x * ROWS;
-    const bool first_cta = blockIdx.x == 0 && hv == 0;
+    // MAPS: B of segments 0 .. P - 2, then M of 1 .. P - 2; OUTPUTS: segments 0 .. P - 1
+    const int parts = PHASE == WHOLE ? 1 : PHASE == MAPS ? 2 * a.segments - 3 : a.segments, sequence = blockIdx.z / parts, part = blockIdx.z % parts;
+    const bool identity = PHASE == MAPS && part >= a.segments - 1, first_cta = blockIdx.x == 0 && hv == 0 && part == 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const Sequence seq = read_sequence(a, blockIdx.z, first_cta);
+    Sequence seq = read_sequence(a, sequence, first_cta);
     if (!seq.live) return;                                                          // (the whole CTA)
-    if (__syncthreads_or(taken_before(a, blockIdx.z, seq, tid, Z::THREADS))) {
-        if (first_cta && tid == 0) report_taken(a, blockIdx.z);
+    if (__syncthreads_or(taken_before(a, sequence, seq, tid, Z::THREADS))) {
+        if (first_cta && tid == 0) report_taken(a, sequence);
         return;
     }
+    const Segment seg = segment_of(seq.length, identity ? part - a.segments + 2 : part, PHASE == WHOLE ? 1 : a.segments, D, a.dv, (int)sizeof(T));
+    if (seg.count == 1 ? PHASE == MAPS || seg.p > 0 : identity && blockIdx.x > 0) return;
+    seq.begin += seg.begin;
+    seq.length = seg.length;
     const int n = (seq.length + C - 1) / C;                                         // chunks
     if (tid == 0) {
         for (int s = 0; s < 3; ++s) {
@@ -472,7 +506,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         if constexpr (Z::SPLIT_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Z::CHAIN_REGS));
         constexpr int G = Z::GROUPS, H = D / G, HB = H / 16, TG = C / G, TB = TG / 16;      // a thread's part of its row and of the tokens, in blocks of 16
         const int c = (warp >> 2) - Z::PREPS, r = (warp & 3) * 32 + lane;
-        const bool is_row = row_base + r < a.dv;
+        const bool is_row = identity ? r < D : row_base + r < a.dv;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem_base + lanes + c * H, z_at = tmem_base + lanes + Z::Z_COL + TG * c, d_at = tmem_base + lanes + Z::D_COL + TG * c;
         const bool issuer = warp == 4 * Z::PREPS, leader = issuer && lane == 0;
@@ -492,11 +526,23 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         float S[H], m = 0.f, inv_row = 1.f, scale_row = 1.f;
 #pragma unroll
         for (int e = 0; e < H; e += 4) {
-            const float4 x = is_row && !seq.fresh ? __ldcs(reinterpret_cast<const float4*>(state + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (PHASE == OUTPUTS && seg.count > 1) {
+                if (is_row) x = __ldcs(scratch<T>(a, seq.begin, hv, (row_base + r) * D + c * H + e));
+            } else if (identity) {
+                const int at = c * H + e;
+                x = make_float4(r == at, r == at + 1, r == at + 2, r == at + 3);
+            } else if (is_row && !seq.fresh && seg.p == 0) {
+                x = __ldcs(reinterpret_cast<const float4*>(state + e));
+            }
             S[e] = x.x; S[e + 1] = x.y; S[e + 2] = x.z; S[e + 3] = x.w;
         }
 #pragma unroll
         for (int e = 0; e < H; e += 2) m = max3(m, S[e], S[e + 1]);
+        if (PHASE == MAPS && seg.p == 0 && is_row) {              // (OUTPUTS' last segment may be done with the state before its first one begins)
+#pragma unroll
+            for (int e = 0; e < H; e += 4) *scratch<T>(a, seq.begin, hv, (row_base + r) * D + c * H + e) = make_float4(S[e], S[e + 1], S[e + 2], S[e + 3]);
+        }
         *mine = m;
         meet();
         int issued = 0;                                           // chunks whose last products have been issued
@@ -508,9 +554,13 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             float sc;
             // ---- Z = S K^T, and S Q^T ----
             m = of_row(0);
-            if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f)) {
+            if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f && scale_row < 0x1p60f)) {
                 float inv;
                 pow2_scale(m, WIDE, sc, inv);
+                if (sc > 0x1p60f) {                               // (2^-e stays a normal number: a state below 2^-114 loses places, as it would in fp32)
+                    sc = 0x1p60f;
+                    inv = 0x1p-60f;
+                }
 #pragma unroll
                 for (int e = 0; e < H; e += 2) {
                     const float2 y = __fmul2_rn(pair(S[e], S[e + 1]), pair(sc, sc));
@@ -559,7 +609,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
                 for (int e = 0; e < TG; ++e) {
                     const int t = i * C + TG * c + e;
-                    val[e] = is_row && t < seq.length ? __ldg(reinterpret_cast<const float*>(vp + t * a.v_stride)) : 0.f;
+                    val[e] = is_row && !identity && t < seq.length ? __ldg(reinterpret_cast<const float*>(vp + t * a.v_stride)) : 0.f;
                 }
             }
             wait_mma(bar_z, turn);
@@ -712,9 +762,17 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             if (meet()) { fail = true; break; }
         }
         if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
-        if (!fail && is_row) {
+        const bool last = PHASE == OUTPUTS && seg.p == seg.count - 1;
+        if (!fail && is_row && (PHASE != OUTPUTS || last)) {
+            const long long next_row = seq.begin + seq.length;    // of the next segment: where a map goes
+            int to_at = (identity ? a.dv * D + r * D : (row_base + r) * D) + c * H;
+            asm volatile("" : "+r"(to_at));                       // (not to be worked out ahead of the loop, which needs the registers)
 #pragma unroll
-            for (int e = 0; e < H; e += 4) __stcs(reinterpret_cast<float4*>(state + e), make_float4(S[e] * inv_row, S[e + 1] * inv_row, S[e + 2] * inv_row, S[e + 3] * inv_row));
+            for (int e = 0; e < H; e += 4) {
+                float4* to = reinterpret_cast<float4*>(state + e);
+                if (PHASE == MAPS) to = scratch<T>(a, next_row, hv, to_at + e);
+                *to = make_float4(S[e] * inv_row, S[e + 1] * inv_row, S[e + 2] * inv_row, S[e + 3] * inv_row);
+            }
         }
     } else {
         // =============================== VALUES IN, OUTPUTS OUT ===============================
@@ -730,7 +788,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
             for (int x = 0; x < C * CH / 128; ++x) {
                 const int item = x * 128 + ot, t = item / CH, ch = item % CH, token = i * C + t;
-                const bool there = token < seq.length && ch * VEC < rows;
+                const bool there = token < seq.length && ch * VEC < rows && !identity;
                 const uint32_t dst = smem_u32(v_s + t * ROWS + ch * VEC);
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(there ? vp + token * a.v_stride + ch * VEC : vp), "r"(there ? 16 : 0) : "memory");
             }
@@ -759,7 +817,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             // read out first and stored behind that, so that the chain may go on (fp32: half of it, for want of registers)
             constexpr int PER = sizeof(T) == 2 ? 2 : 1, FIRST = PER == 2 ? 0 : 2;      // outputs per register; blocks of 16 stored at once
             T* dst = op + (long long)(i * C) * a.out_stride;
-            const int left = is_row ? seq.length - i * C : 0;
+            const int left = is_row && PHASE != MAPS ? seq.length - i * C : 0;
             uint32_t o[(4 - FIRST) * 16 / PER];
             auto block = [&](int b, uint32_t* to) {
                 uint32_t v[16], w[16];
@@ -802,16 +860,66 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             arrive(bar_tfree(i));
         }
     }
-    if (fail && a.status && atomicCAS(a.status, ONELA_OK, ONELA_E_TIMEOUT) == ONELA_OK) a.status[1] = blockIdx.z;
+    if (fail && a.status && atomicCAS(a.status, ONELA_OK, ONELA_E_TIMEOUT) == ONELA_OK) a.status[1] = sequence;
     tc_fence_before();
     __syncthreads();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(Z::TMEM_COLS) : "memory");
 }
 
+// The states before segments 2 .. P - 1 of a cut sequence: S <- S M_p + B_p, p = 1 .. P - 2, from the state before segment 1, each in the place of its B.  A
+// CTA has 16 rows of the state, which need no others; S in shared memory, M from L2, fp32 throughout.  What bounds it: the shared memory's
+// broadcasts, about 2 us a segment.
+constexpr int FOLD_ROWS = 16, FOLD_THREADS = 128;
 template <int D, typename T>
-cudaError_t launch_dt(const DeltaArgs& a, cudaStream_t stream) {
+__global__ void __launch_bounds__(FOLD_THREADS) delta_fold_kernel(const DeltaArgs a) {
+    constexpr int GROUPS = FOLD_THREADS / D, OWN = FOLD_ROWS / GROUPS;              // threads per column; rows per thread
+    __shared__ __align__(16) float S_s[FOLD_ROWS][D];
+    const int hv = blockIdx.y, row0 = blockIdx.x * FOLD_ROWS, col = threadIdx.x % D, own0 = threadIdx.x / D * OWN;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Sequence seq = read_sequence(a, blockIdx.z, false);
+    if (!seq.live || __syncthreads_or(taken_before(a, blockIdx.z, seq, threadIdx.x, FOLD_THREADS))) return;
+    if (segment_of(seq.length, 0, a.segments, D, a.dv, (int)sizeof(T)).count == 1) return;
+    auto row_of = [&](int p) { return seq.begin + segment_of(seq.length, p, a.segments, D, a.dv, (int)sizeof(T)).begin; };
+    for (int x = threadIdx.x; x < FOLD_ROWS * D / 4; x += FOLD_THREADS)             // the state before segment 1
+        *reinterpret_cast<float4*>(&S_s[0][0] + 4 * x) = *scratch<T>(a, row_of(1), hv, row0 * D + 4 * x);
+    for (int p = 1; p + 1 < a.segments; ++p) {
+        const long long at = row_of(p + 1);                                         // where M_p and B_p lie
+        __syncthreads();
+        float acc[OWN];
+#pragma unroll
+        for (int r = 0; r < OWN; ++r) {
+            const int e = (row0 + own0 + r) * D + col;
+            acc[r] = reinterpret_cast<const float*>(scratch<T>(a, at, hv, e & ~3))[e & 3];
+        }
+#pragma unroll 4
+        for (int k = 0; k < D; k += 4) {
+            float m[4];
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const int e = a.dv * D + (k + f) * D + col;
+                m[f] = reinterpret_cast<const float*>(scratch<T>(a, at, hv, e & ~3))[e & 3];
+            }
+#pragma unroll
+            for (int r = 0; r < OWN; ++r) {
+                const float4 x = *reinterpret_cast<const float4*>(&S_s[own0 + r][k]);
+                acc[r] = fmaf(x.x, m[0], fmaf(x.y, m[1], fmaf(x.z, m[2], fmaf(x.w, m[3], acc[r]))));
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < OWN; ++r) {
+            const int e = (row0 + own0 + r) * D + col;
+            S_s[own0 + r][col] = acc[r];
+            reinterpret_cast<float*>(scratch<T>(a, at, hv, e & ~3))[e & 3] = acc[r];
+        }
+    }
+}
+
+template <int D, typename T, int PHASE>
+cudaError_t launch_phase(const DeltaArgs& a, int parts, cudaStream_t stream) {
     using Z = Shape<D, T>;
-    auto kern = delta_chunk_kernel<D, T>;
+    auto kern = delta_chunk_kernel<D, T, PHASE>;
     constexpr int MAX_DEVICES = 64;
     static std::mutex setup_mutex;
     static bool ready[MAX_DEVICES] = {};
@@ -825,7 +933,15 @@ cudaError_t launch_dt(const DeltaArgs& a, cudaStream_t stream) {
             ready[dev] = true;
         }
     }
-    return launch_dependent(kern, dim3((a.dv + ROWS - 1) / ROWS, a.Hv, a.num_sequences), dim3(Z::THREADS), Z::SMEM, stream, a);
+    return launch_dependent(kern, dim3((a.dv + ROWS - 1) / ROWS, a.Hv, a.num_sequences * parts), dim3(Z::THREADS), Z::SMEM, stream, a);
+}
+template <int D, typename T>
+cudaError_t launch_dt(const DeltaArgs& a, cudaStream_t stream) {
+    if (a.segments == 1) return launch_phase<D, T, WHOLE>(a, 1, stream);
+    cudaError_t e = launch_phase<D, T, MAPS>(a, 2 * a.segments - 3, stream);
+    if (e == cudaSuccess && a.segments > 2)
+        e = launch_dependent(delta_fold_kernel<D, T>, dim3(a.dv / FOLD_ROWS, a.Hv, a.num_sequences), dim3(FOLD_THREADS), 0, stream, a);
+    return e == cudaSuccess ? launch_phase<D, T, OUTPUTS>(a, a.segments, stream) : e;
 }
 template <int D>
 cudaError_t launch_d(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
@@ -836,7 +952,20 @@ cudaError_t launch_d(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
 
 bool delta_chunk_supported(int32_t dk, int32_t) { return dk == 32 || dk == 64 || dk == 128; }
 
-cudaError_t launch_delta_chunk(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
+// Segments.  A chunk takes every CTA about the same time, whatever shares the GPU; one CTA fits an SM.  P segments of n chunks cost ceil(n / P) chunks twice,
+// the fold a third of a chunk per segment and the launches about two; MAPS has 2 P - 3 CTAs per chain.
+cudaError_t launch_delta_chunk(DeltaArgs a, int32_t dtype, long long longest, cudaStream_t stream) {
+    constexpr int SMS = 148, MOST = 16;
+    const long long chains = (long long)((a.dv + ROWS - 1) / ROWS) * a.Hv * a.num_sequences, chunks = (longest + C - 1) / C;
+    double best = (double)chunks;
+    // (one block of rows only: another one's outputs would overwrite what a state's second block has yet to read)
+    for (int p = 3; p <= MOST && a.dv <= ROWS && chains * (2 * p - 3) <= SMS && chunks / p >= least_chunks(a.dk, a.dv, dtype == ONELA_DTYPE_BF16 ? 2 : 4); ++p) {
+        const double cost = 2.0 * (double)((chunks + p - 1) / p) + (p - 2) / 3.0 + 3.0;
+        if (cost < best) {
+            best = cost;
+            a.segments = p;
+        }
+    }
     return a.dk == 32 ? launch_d<32>(a, dtype, stream) : a.dk == 64 ? launch_d<64>(a, dtype, stream) : launch_d<128>(a, dtype, stream);
 }
 

@@ -147,6 +147,63 @@ def test_both_kernels_agree_with_the_recurrence_when_the_hint_is_wrong(max_token
     _case([150, 1, 33], max_tokens=max_tokens, dk=128, dv=128, dtype="bf16")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dk,dv,H", [(128, 128, 2), (64, 64, 1), (64, 128, 2), (128, 64, 1), (32, 32, 3), (64, 96, 1)])
+@pytest.mark.parametrize("lens,fresh", [([2500], [0]), ([1300, 40, 0, 2111], [1, 0, 1, 0])])
+def test_long_prompts_of_few_heads(dk, dv, H, lens, fresh, dtype):
+    """Sequences that are cut into segments, beside ones that are too short for it."""
+    _case(lens, dk=dk, dv=dv, H=H, dtype=dtype, fresh=fresh, slots=[len(lens) - i for i in range(len(lens))])
+
+
+@pytest.mark.parametrize("gates,memory", [((1.0, 1.0), 1500), ((0.98, 1.0), 200), ((0.0, 1.0), 20)])
+def test_gates_of_long_prompts(gates, memory):
+    for dtype in ("fp32", "bf16"):
+        _case([1500], dk=128, dv=128, H=2, dtype=dtype, gates=gates, memory=memory)
+
+
+@pytest.mark.parametrize("H,N", [(2, 1500), (40, 400)])
+def test_states_that_fade_away_and_come_back(H, N):
+    """Gates of about 0.4 and no values for most of the sequence: the state passes every exponent down to nothing (and so does the map of a segment),
+    then values come again."""
+    b = Batch([N], H=H, dk=128, dv=128, dtype="fp32", gates=(0.3, 0.5))
+    b.v[:N - 90] = 0
+    ref, slots = b.reference()
+    b.run()
+    torch.cuda.synchronize()
+    assert torch.isfinite(b.out).all() and torch.isfinite(b.states).all()
+    tail = {t: o for t, o in ref[0].items() if t >= N - 80}
+    got = b.out.double().cpu().numpy()
+    for t, o in tail.items():
+        for h in range(0, H, 7):
+            assert np.linalg.norm(got[t, h] - o[h]) <= 16 * 20 * 2.0 ** -24 * max(np.linalg.norm(o[h]), np.linalg.norm(ref[1][0, h]) / np.sqrt(128)), (t, h)
+    assert np.linalg.norm(b.states[0].double().cpu().numpy() - ref[1][0]) <= 16 * 20 * 2.0 ** -24 * np.linalg.norm(ref[1][0])
+
+
+def test_cut_prompts_in_strided_outputs_and_captured():
+    """The segments' states lie in the rows of `out` meanwhile: what lies between the rows is not touched, and a replay does the same work."""
+    b = Batch([1700, 90], H=2, dk=128, dv=128, dtype="bf16")
+    ref, slots = b.reference()
+    N = b.q.shape[0]
+    outs = torch.full((N, 6, 128), UNTOUCHED, dtype=torch.bfloat16, device="cuda")
+    b.out, first = outs[:, 2:4], b.states.clone()
+    b.run()
+    torch.cuda.synchronize()
+    b.check(ref, slots)
+    assert torch.all(outs[:, :2] == UNTOUCHED) and torch.all(outs[:, 4:] == UNTOUCHED)
+    want = [b.out.clone(), b.states.clone()]
+    args = dict(starts=b.starts, slots=b.i32(b.slots))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.run(**args)
+    for _ in range(3):
+        b.states.copy_(first)
+        b.out.fill_(5.0)
+        b.out[1790:] = UNTOUCHED
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b.out, want[0]) and torch.equal(b.states, want[1])
+
+
 def test_no_starts_no_slots():
     b = Batch([1] * 5, extra_rows=0, extra_states=0, dk=128, dv=128, dtype="bf16")
     ref, slots = b.reference()
