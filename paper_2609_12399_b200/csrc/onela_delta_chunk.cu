@@ -867,13 +867,16 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 }
 
 // The states before segments 2 .. P - 1 of a cut sequence: S <- S M_p + B_p, p = 1 .. P - 2, from the state before segment 1, each in the place of its B.  A
-// CTA has 16 rows of the state, which need no others; S in shared memory, M from L2, fp32 throughout.  What bounds it: the shared memory's
-// broadcasts, about 2 us a segment.
-constexpr int FOLD_ROWS = 16, FOLD_THREADS = 128;
+// CTA has 16 rows of the state, which need no others; S and M in shared memory, the next M on its way meanwhile, fp32 throughout.  (M read from
+// global memory as it is used: 30 us a segment against MEASURED.)
+constexpr int FOLD_ROWS = 16, FOLD_THREADS = 256;
+template <int D>
+constexpr int fold_smem() { return (2 * D * D + FOLD_ROWS * D) * 4; }
 template <int D, typename T>
 __global__ void __launch_bounds__(FOLD_THREADS) delta_fold_kernel(const DeltaArgs a) {
     constexpr int GROUPS = FOLD_THREADS / D, OWN = FOLD_ROWS / GROUPS;              // threads per column; rows per thread
-    __shared__ __align__(16) float S_s[FOLD_ROWS][D];
+    extern __shared__ __align__(16) float fold_s[];
+    float *M_s = fold_s, *S_s = fold_s + 2 * D * D;                                 // [2][D][D], [FOLD_ROWS][D]
     const int hv = blockIdx.y, row0 = blockIdx.x * FOLD_ROWS, col = threadIdx.x % D, own0 = threadIdx.x / D * OWN;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -881,37 +884,47 @@ __global__ void __launch_bounds__(FOLD_THREADS) delta_fold_kernel(const DeltaArg
     if (!seq.live || __syncthreads_or(taken_before(a, blockIdx.z, seq, threadIdx.x, FOLD_THREADS))) return;
     if (segment_of(seq.length, 0, a.segments, D, a.dv, (int)sizeof(T)).count == 1) return;
     auto row_of = [&](int p) { return seq.begin + segment_of(seq.length, p, a.segments, D, a.dv, (int)sizeof(T)).begin; };
+    auto fetch = [&](int p) {                                                       // M_p, which lies in the rows of segment p + 1
+        const long long at = row_of(p + 1);
+        for (int x = threadIdx.x; x < D * D / 4; x += FOLD_THREADS)
+            sm100::cp_async16(smem_u32(M_s + (p & 1) * D * D + 4 * x), scratch<T>(a, at, hv, a.dv * D + 4 * x));
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fetch(1);
     for (int x = threadIdx.x; x < FOLD_ROWS * D / 4; x += FOLD_THREADS)             // the state before segment 1
-        *reinterpret_cast<float4*>(&S_s[0][0] + 4 * x) = *scratch<T>(a, row_of(1), hv, row0 * D + 4 * x);
+        *reinterpret_cast<float4*>(S_s + 4 * x) = *scratch<T>(a, row_of(1), hv, row0 * D + 4 * x);
     for (int p = 1; p + 1 < a.segments; ++p) {
-        const long long at = row_of(p + 1);                                         // where M_p and B_p lie
-        __syncthreads();
+        const long long at = row_of(p + 1);
         float acc[OWN];
+        float* place[OWN];
 #pragma unroll
         for (int r = 0; r < OWN; ++r) {
             const int e = (row0 + own0 + r) * D + col;
-            acc[r] = reinterpret_cast<const float*>(scratch<T>(a, at, hv, e & ~3))[e & 3];
+            place[r] = reinterpret_cast<float*>(scratch<T>(a, at, hv, e & ~3)) + (e & 3);
+            acc[r] = *place[r];
         }
+        if (p + 2 < a.segments) {
+            fetch(p + 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        } else {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        }
+        __syncthreads();
+        const float* M = M_s + (p & 1) * D * D + col;
 #pragma unroll 4
         for (int k = 0; k < D; k += 4) {
-            float m[4];
-#pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                const int e = a.dv * D + (k + f) * D + col;
-                m[f] = reinterpret_cast<const float*>(scratch<T>(a, at, hv, e & ~3))[e & 3];
-            }
+            const float m0 = M[k * D], m1 = M[(k + 1) * D], m2 = M[(k + 2) * D], m3 = M[(k + 3) * D];
 #pragma unroll
             for (int r = 0; r < OWN; ++r) {
-                const float4 x = *reinterpret_cast<const float4*>(&S_s[own0 + r][k]);
-                acc[r] = fmaf(x.x, m[0], fmaf(x.y, m[1], fmaf(x.z, m[2], fmaf(x.w, m[3], acc[r]))));
+                const float4 x = *reinterpret_cast<const float4*>(S_s + (own0 + r) * D + k);
+                acc[r] = fmaf(x.x, m0, fmaf(x.y, m1, fmaf(x.z, m2, fmaf(x.w, m3, acc[r]))));
             }
         }
-        __syncthreads();
+        __syncthreads();                                                            // S has been read, and M, whose place the one after next takes
 #pragma unroll
         for (int r = 0; r < OWN; ++r) {
-            const int e = (row0 + own0 + r) * D + col;
-            S_s[own0 + r][col] = acc[r];
-            reinterpret_cast<float*>(scratch<T>(a, at, hv, e & ~3))[e & 3] = acc[r];
+            S_s[(own0 + r) * D + col] = acc[r];
+            *place[r] = acc[r];
         }
     }
 }
@@ -938,9 +951,10 @@ cudaError_t launch_phase(const DeltaArgs& a, int parts, cudaStream_t stream) {
 template <int D, typename T>
 cudaError_t launch_dt(const DeltaArgs& a, cudaStream_t stream) {
     if (a.segments == 1) return launch_phase<D, T, WHOLE>(a, 1, stream);
-    cudaError_t e = launch_phase<D, T, MAPS>(a, 2 * a.segments - 3, stream);
-    if (e == cudaSuccess && a.segments > 2)
-        e = launch_dependent(delta_fold_kernel<D, T>, dim3(a.dv / FOLD_ROWS, a.Hv, a.num_sequences), dim3(FOLD_THREADS), 0, stream, a);
+    cudaError_t e = cudaFuncSetAttribute(delta_fold_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, fold_smem<D>());
+    if (e == cudaSuccess) e = launch_phase<D, T, MAPS>(a, 2 * a.segments - 3, stream);
+    if (e == cudaSuccess)
+        e = launch_dependent(delta_fold_kernel<D, T>, dim3(a.dv / FOLD_ROWS, a.Hv, a.num_sequences), dim3(FOLD_THREADS), fold_smem<D>(), stream, a);
     return e == cudaSuccess ? launch_phase<D, T, OUTPUTS>(a, a.segments, stream) : e;
 }
 template <int D>
