@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             // keys (rows 0 - 63) and queries (64 - 127) as the K-major operand tile, every row with its own power of two; tokens
             // beyond the sequence are zeros with alpha = 1, beta = 0: they change nothing
             const int lr = pt % LR, row0 = pt / LR;
-#pragma unroll
+#pragma unroll 1
             for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
                 uint4 raw[BATCH][NC];
 #pragma unroll
@@ -784,31 +784,36 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         const T* vp = static_cast<const T*>(a.v) + seq.begin * a.v_stride + (long long)hv * a.dv + row_base;
         T* op = static_cast<T*>(a.out) + seq.begin * a.out_stride + (long long)hv * a.dv + row_base + r;
         constexpr int VEC = Vec16<T>::N, CH = ROWS / VEC;         // 16-byte chunks per token
+        const int v_token = ot / CH, v_chunk = ot % CH;           // this thread's of the first 128 / CH tokens
+        const long long v_step = a.v_stride * (128 / CH), out_step = a.out_stride;
         auto load_values = [&](int i) {
-#pragma unroll
+            const T* from = vp + (long long)(i * C + v_token) * a.v_stride + v_chunk * VEC;
+            uint32_t dst = smem_u32(v_s + v_token * ROWS + v_chunk * VEC);
+            int left = v_chunk * VEC < rows && !identity ? seq.length - i * C - v_token : 0;
+#pragma unroll 2
             for (int x = 0; x < C * CH / 128; ++x) {
-                const int item = x * 128 + ot, t = item / CH, ch = item % CH, token = i * C + t;
-                const bool there = token < seq.length && ch * VEC < rows && !identity;
-                const uint32_t dst = smem_u32(v_s + t * ROWS + ch * VEC);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(there ? vp + token * a.v_stride + ch * VEC : vp), "r"(there ? 16 : 0) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(left > 0 ? from : vp), "r"(left > 0 ? 16 : 0) : "memory");
+                from += v_step;
+                dst += 128 / CH * ROWS * (int)sizeof(T);
+                left -= 128 / CH;
             }
             asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
             arrive(bar_v);
         };
-        if (Z::STAGE_V && n > 0) load_values(0);
 #pragma unroll 1
-        for (int i = 0; i < n && !fail; ++i) {
+        for (int i = -1; i < n && !fail; ++i) {                   // (-1: the first values only)
             const uint32_t turn = i & 1;
-            const float* kco = kco_s + i % Z::K_STAGES * Z::KCO + C;
-            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO + C;
+            const float* kco = kco_s + max(i, 0) % Z::K_STAGES * Z::KCO + C;
+            const float* tco = tco_s + max(i, 0) % Z::T_STAGES * Z::TCO + C;
             if (Z::STAGE_V && i + 1 < n) {
-                wait(bar_vfree, turn);
+                if (i >= 0) wait(bar_vfree, turn);
                 if (!fail) load_values(i + 1);
             }
             if (!Z::STAGE_V && i + 1 < n) {                           // the lines of the next chunk's values into L2
                 const int t = min((i + 1) * C + (ot >> 1), seq.length - 1);
                 for (int x = (ot & 1) * 32; x < rows; x += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(vp + t * a.v_stride + x));
             }
+            if (i < 0) continue;
             wait(bar_o, turn);
             // (the warps of this team do not wait for one another; a warp's threads leave together)
             if (__any_sync(0xffffffffu, fail)) { fail = true; break; }
@@ -839,11 +844,15 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             auto store = [&](int first, int count, const uint32_t* from) {
 #pragma unroll
                 for (int e = 0; e < count; ++e) {
-                    if (first + e < left) {
-                        if constexpr (PER == 2) *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(from[e / 2] >> (16 * (e & 1)));
-                        else *dst = __uint_as_float(from[e]);
-                    }
-                    dst += a.out_stride;
+                    // (predicated, not branched around: a third of the code)
+                    if constexpr (PER == 2)
+                        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\t@p st.global.b16 [%0], %1;\n\t}" ::"l"(dst),
+                                     "h"((uint16_t)(from[e / 2] >> (16 * (e & 1)))), "r"(first + e), "r"(left)
+                                     : "memory");
+                    else
+                        asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %2, %3;\n\t@p st.global.b32 [%0], %1;\n\t}" ::"l"(dst), "r"(from[e]), "r"(first + e), "r"(left)
+                                     : "memory");
+                    dst += out_step;
                 }
             };
 #pragma unroll 1
