@@ -57,7 +57,7 @@ using sm100::umma_desc;
 constexpr int ROWS = 128;                 // state rows per CTA
 constexpr int KQ_BLOCK = 2 * TILE;        // 128 rows (64 of K, 64 of Q) of 64 fp16
 constexpr int NARROW = 3, WIDE = 12;      // largest elements of operand rows: K, Q, T, P in [2^3, 2^4), S, X, D in [2^12, 2^13)
-constexpr int CHAIN_BARRIER = 3;          // named barrier (1, 2: the preparing teams')
+constexpr int CHAIN_BARRIER = 3, OUT_BARRIER = 4;      // named barriers (1, 2: the preparing teams')
 
 template <int D, typename T>
 struct Shape {
@@ -70,12 +70,13 @@ struct Shape {
     static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK, T_BYTES = 2 * TILE, P_BYTES = PARTS * TILE;
     static constexpr bool STAGE_V = !WIDE_T;                       // values through shared memory (fp32: there is no room)
     static constexpr int V_BYTES = STAGE_V ? C * ROWS * (int)sizeof(T) : 0;
+    static constexpr int O_TOKENS = 32, O_BYTES = WIDE_T ? 0 : O_TOKENS * ROWS * 2;      // outputs on their way out (bf16)
     static constexpr int A_BYTES = (C * AP * 4 + 1023) / 1024 * 1024, X_BYTES = 5 * 1024;
     // per K stage: beta g / key scale, g / query scale, beta, g_C; per T stage: weights of D's columns for the state, what undoes P's rows' scales
     // and T's
     static constexpr int KCO = 3 * C + 4, TCO = 2 * C + 4;
     static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + (2 * GROUPS + 4) * ROWS) * 4 + 256;
-    static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
+    static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + O_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
     static_assert(SMEM <= 232448, "shared memory");
     // tensor memory: S operand / D K | Z, X operand, D operand for the outputs (64) ; S Q^T (64) | D (64) | D P^T (64) | per preparing team 64
     static constexpr uint32_t Z_COL = 128, O1_COL = Z_COL + C, D_COL = 256, O2_COL = 320, PREP_COL = 384, TMEM_COLS = 512;
@@ -129,7 +130,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
     uint8_t* p_ring = t_ring + Z::T_STAGES * Z::T_BYTES;
     uint8_t* prep_s = p_ring + Z::T_STAGES * Z::P_BYTES;                            // per preparing team: matrix, scratch
     T* v_s = reinterpret_cast<T*>(prep_s + Z::PREPS * (Z::A_BYTES + Z::X_BYTES));   // [token][row]
-    float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);
+    uint16_t* o_s = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);       // [token][row]
+    float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(o_s) + Z::O_BYTES);
     float* tco_s = kco_s + Z::K_STAGES * Z::KCO;
     float* tok_s = tco_s + Z::T_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
     float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [2][GROUPS][ROWS] largest of a row's part: S, X, D in turn; D as weighted
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         const uint32_t acc_at = uniform(tmem_base + Z::PREP_COL + team * C);
         constexpr int VEC = Vec16<T>::N, CPR = D / VEC, LR = CPR < 8 ? CPR : 8;      // 16-byte chunks and lanes per row
         constexpr int PASS_ROWS = 128 / LR, PASSES = 128 / PASS_ROWS, NC = CPR / LR;
-        constexpr int BATCH = PASSES * NC > 8 ? 8 / NC : PASSES;                     // passes whose loads are in flight together
+        constexpr int BATCH = PASSES * NC > 4 ? 4 / NC : PASSES;                     // passes whose loads are in flight together
         const T* kp = static_cast<const T*>(a.k) + seq.begin * a.k_stride + (long long)hk * D;
         const T* qp = static_cast<const T*>(a.q) + seq.begin * a.q_stride + (long long)hk * D;
         auto gate_of = [&](const float* g, int t, float pad) { return t < seq.length ? __ldg(g + (seq.begin + t) * a.gate_stride + hv) : pad; };
@@ -782,7 +784,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int rows = min(ROWS, a.dv - row_base);              // a multiple of 32
         const T* vp = static_cast<const T*>(a.v) + seq.begin * a.v_stride + (long long)hv * a.dv + row_base;
-        T* op = static_cast<T*>(a.out) + seq.begin * a.out_stride + (long long)hv * a.dv + row_base + r;
+        T* out0 = static_cast<T*>(a.out) + seq.begin * a.out_stride + (long long)hv * a.dv + row_base;
+        T* op = out0 + r;
         constexpr int VEC = Vec16<T>::N, CH = ROWS / VEC;         // 16-byte chunks per token
         const int v_token = ot / CH, v_chunk = ot % CH;           // this thread's of the first 128 / CH tokens
         const long long v_step = a.v_stride * (128 / CH), out_step = a.out_stride;
@@ -815,8 +818,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             }
             if (i < 0) continue;
             wait(bar_o, turn);
-            // (the warps of this team do not wait for one another; a warp's threads leave together)
-            if (__any_sync(0xffffffffu, fail)) { fail = true; break; }
+            if (bar_or(OUT_BARRIER, 128, fail ? 1 : 0)) { fail = true; break; }
             tc_fence_after();
             const float inv_row = inv_s[turn * ROWS + r], inv_d = inv_s[(2 + turn) * ROWS + r];
             // read out first and stored behind that, so that the chain may go on (fp32: half of it, for want of registers)
@@ -864,7 +866,26 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             for (int b = FIRST; b < 4; ++b) block(b, o + (b - FIRST) * 16 / PER);
             tc_fence_before();
             arrive(bar_ofree);
-            store(16 * FIRST, C - 16 * FIRST, o);
+            if constexpr (PER == 2) {
+                // through shared memory: a thread has a row of the state, memory wants a token's rows side by side.  (Two bytes per thread and token
+                // straight to memory were twice the code, and code is what limits two SMs that share an instruction cache.)
+                const int there = PHASE == MAPS ? 0 : seq.length - i * C;
+#pragma unroll
+                for (int t0 = 0; t0 < C; t0 += Z::O_TOKENS) {
+#pragma unroll
+                    for (int e = 0; e < Z::O_TOKENS; ++e) o_s[e * ROWS + r] = (uint16_t)(o[(t0 + e) / 2] >> (16 * (e & 1)));
+                    bar_or(OUT_BARRIER, 128, 0);
+#pragma unroll 1
+                    for (int x = ot; x < Z::O_TOKENS * ROWS / 8; x += 128) {
+                        const int t = x / (ROWS / 8), ch = x % (ROWS / 8) * 8;
+                        if (t0 + t < there && ch < rows)
+                            *reinterpret_cast<uint4*>(out0 + (long long)(i * C + t0 + t) * a.out_stride + ch) = *reinterpret_cast<const uint4*>(o_s + t * ROWS + ch);
+                    }
+                    bar_or(OUT_BARRIER, 128, 0);
+                }
+            } else {
+                store(16 * FIRST, C - 16 * FIRST, o);
+            }
             arrive(bar_kfree(i));
             arrive(bar_tfree(i));
         }
