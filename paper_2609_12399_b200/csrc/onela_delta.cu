@@ -8,6 +8,9 @@
 // Many tokens: the chain of a token's latencies (the next token's inputs are on their way meanwhile), so long sequences go to the
 // chunked kernel (onela_delta_chunk.cu).
 //
+// Measured: 64 sequences x 32 heads of 128 x 128, one token, 43.5 us (5.9 TB/s, 0.92 of the measured copy); 16 heads of one sequence 3.7 us, a launch;
+// 37 sequences x 16 heads of 64 x 64 fp32, five tokens, 9.5 us.
+//
 // A lane group works on PASSES rows.  Four, so that a warp has 4 x 512 bytes x 4 of state in flight, where the call fills the GPU; one,
 // four times the CTAs, where it does not.
 #include <algorithm>

@@ -8,14 +8,16 @@
 // A row lies in the shared memory of one cluster of 1 to 8 CTAs, read from memory once.  Masses are integers, w in units of 2^-F with F = 62 -
 // ceil(log2 vocab) (43 places or more), so sums are exact in any order, atomics included.  w = 2^(n / 256 + f / 256) in 64 bits, |f| <= 1 / 2:
 // 2^(n mod 256 / 256) from a table, the rest by its series to the third power (Tang 1989; relative error 2e-13).  (64 rows of 100 003 logits without
-// filters: exp() 40 us over a pass that only looks for the largest, this 10.5, the same on sums of two fp32 numbers, 36 instructions, 21, with the
-// conversions from and to 64 bits done on the bits 14.)
+// filters take 9 us more than a pass that only looks for the largest; the same on sums of two fp32 numbers, 36 instructions, 21, with the conversions
+// from and to 64 bits done on the bits 14.)
 //   top-k   tokens counted by bins of their distance from the largest (896 of them); the bin in which the count passes k is cut
 //           into 512 bins of the values' bit patterns, and so on until a bin holds one token or one value
 //   top-p   the same descent on the bins' masses, from the same first histogram, towards top_p times the mass of the top-k tokens.  (Counts alone in the
-//           first histogram, the masses around a guessed bin by a pass of their own: 86 us against MEASURED for 64 rows of 100 003.)
+//           first histogram, the masses around a guessed bin by a pass of their own: 86 us against 69 for 64 rows of 100 003.)
 // A histogram is reduced by the cluster (a CTA sums a share of the bins over all CTAs and hands the sums to all), two cluster barriers.
-// What bounds it: launches of a few rows the chain of barriers, many rows the exponentials' and the histogram's instructions.
+// The draw: kept masses by warps (a warp has a run of neighbours), then the one run that passes the target token by token.
+// What bounds it: launches of a few rows the chain of barriers (one row of 131 072 with top-k and top-p 34 us, 12 without filters), many rows the
+// exponentials' and the histogram's instructions (64 rows of 100 003: 14 us to find the largest, 23 without filters, 66 with top-p and min-p).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -47,7 +49,7 @@ struct SampleArgs {
 };
 
 // The first histogram has BINS bins, finer ones FINE.  (As small as this so that two CTAs hold 100 000 fp32 logits: by four 64 rows are
-// two waves, 86 us instead of 54.)
+// two waves, 101 us instead of 74.)
 struct Histograms {
     uint32_t count[BINS], low[BINS], high[BINS];      // this CTA's; a mass's two halves
     u64 all_mass[BINS], fine_mass[FINE];              // the cluster's, of the first and of a finer one
@@ -270,8 +272,8 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         for (int b = tid; b < BINS; b += threads) hist->count[b] = hist->low[b] = hist->high[b] = 0;
         __syncthreads();
     };
-    auto add = [&](int b, u64 m) {
-        atomicAdd(&hist->count[b], 1u);
+    auto add = [&](int b, u64 m, bool counts) {
+        if (counts) atomicAdd(&hist->count[b], 1u);
         if (m == 0) return;
         const uint32_t low = (uint32_t)m, old = atomicAdd(&hist->low[b], low);
         const uint32_t high = (uint32_t)(m >> 32) + (old + low < old);
@@ -360,7 +362,9 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         Cut c{bin, bin_from(r, bin), bin_to(r, bin), 0u, 0u, 0u};
         c.low = key_of<T>(c.from);
         c.high = key_of<T>(c.to);
-        while (count > 1 && c.low != c.high) {
+        bool counted = use_k;                                                      // (the first histogram counts for top-k only)
+        while (!counted || (count > 1 && c.low != c.high)) {
+            counted = true;
             const uint32_t range = c.high - c.low;                                 // bins of 2^shift keys, from the largest down
             const int shift = range < FINE ? 0 : 32 - __clz(range) - 9;
             clear();
@@ -371,7 +375,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
                     const bool near = x[e] >= c.from && x[e] <= c.to;
                     if (!__any_sync(0xffffffffu, near)) continue;
                     const uint32_t key = key_of<T>(x[e]);
-                    if (near && key - c.low <= range && first_bin(r, x[e]) == c.bin) add((int)((c.high - key) >> shift), by_mass ? mass(r, table_s, x[e]) : 0);
+                    if (near && key - c.low <= range && first_bin(r, x[e]) == c.bin) add((int)((c.high - key) >> shift), by_mass ? mass(r, table_s, x[e]) : 0, true);
                 }
             });
             reduce(true, by_mass);
@@ -402,7 +406,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     Cut cut{-1, 0.f, 0.f, 0u, 0u, 0u};
     if (!nothing && !r.greedy && (use_k || use_p)) {
         clear();
-        if (use_p) each_token([&](float x) { add(first_bin(r, x), mass(r, table_s, x)); });
+        if (use_p) each_token([&](float x) { add(first_bin(r, x), mass(r, table_s, x), use_k); });
         else each_token([&](float x) { atomicAdd(&hist->count[first_bin(r, x)], 1u); });
         reduce(false, use_p);
         u64 kept;
