@@ -348,7 +348,7 @@ onela_status onela_delta_rule(const onela_delta_rule_args* args, void* stream);
  * +inf only those are kept; -0 equals +0.  A uniform outside [0, 1) is taken as the nearer end, NaN as 0.  A row that has nothing above -inf gets token -1 and
  * logprob -inf.  vocab up to 360 000, else ONELA_E_CAPACITY. */
 typedef struct onela_sample_args {
-    const void* logits_dev;                  /* [rows][vocab] in dtype, logits_stride elements from row to row (any) */
+    const void* logits_dev;                  /* [rows][vocab] in dtype, logits_stride elements from row to row (any; 0: one row for all) */
     const float *uniforms_dev;               /* [rows] */
     const float *temperature_dev, *top_p_dev, *min_p_dev;   /* [rows] or null: 1, off, off */
     const int32_t* top_k_dev;                /* [rows] or null: off */

@@ -16,8 +16,9 @@
 //           first histogram, the masses around a guessed bin by a pass of their own: 86 us against 69 for 64 rows of 100 003.)
 // A histogram is reduced by the cluster (a CTA sums a share of the bins over all CTAs and hands the sums to all), two cluster barriers.
 // The draw: kept masses by warps (a warp has a run of neighbours), then the one run that passes the target token by token.
-// What bounds it: launches of a few rows the chain of barriers (one row of 131 072 with top-k and top-p 34 us, 12 without filters), many rows the
-// exponentials' and the histogram's instructions (64 rows of 100 003: 14 us to find the largest, 23 without filters, 66 with top-p and min-p).
+// What bounds it: launches of a few rows the chain of barriers (one row of 131 072 with top-k and top-p 29 us, 11.5 without filters; the code, which a launch runs
+// once, counts: loops rolled, 152 -> 128 KB, took 2 us off), many rows the
+// exponentials' and the histogram's instructions (64 rows of 100 003: 13 us to find the largest, 22 without filters, 64 with top-p and min-p).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     };
     // whole vectors, eight on their way at a time; the row's first and last one by elements
     const int whole0 = unit0 == 0 && skip > 0 ? 1 : 0, whole1 = n / VE - (unit0 + n / VE == units && end % VE != 0 ? 1 : 0);
-    constexpr int BATCH = 8;
+    constexpr int BATCH = 4;
     for (int u0 = whole0 + tid; u0 < whole1; u0 += threads * BATCH) {
         uint4 raw[BATCH];
 #pragma unroll
@@ -235,6 +236,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     auto reduce = [&](bool fine, bool masses) {
         sync();
         const int share = (fine ? FINE : BINS) / ctas;
+#pragma unroll 1
         for (int b = tid; b < share; b += threads) {
             const int at = rank * share + b;
             uint32_t count[MAX_CLUSTER], low[MAX_CLUSTER], high[MAX_CLUSTER];
@@ -269,6 +271,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     };
     static_assert(BINS % MAX_CLUSTER == 0 && FINE % MAX_CLUSTER == 0, "shares");
     auto clear = [&] {
+#pragma unroll 1
         for (int b = tid; b < BINS; b += threads) hist->count[b] = hist->low[b] = hist->high[b] = 0;
         __syncthreads();
     };
@@ -286,11 +289,13 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
         const uint32_t* counts = fine ? hist->fine_count : hist->all_count;
         const u64* masses = fine ? hist->fine_mass : hist->all_mass;
         u64 count = 0, m = 0, all;
+#pragma unroll 1
         for (int b = at; b < min(bins, at + per); ++b) {
             count += counts[b];
             m += masses[b];
         }
         u64 before = base0 + block_exclusive_scan<u64>(by_mass ? m : count, scan64_s, &all);
+#pragma unroll 1
         for (int b = at; b < min(bins, at + per); ++b) {
             const u64 step = by_mass ? masses[b] : counts[b];
             const bool here = by_mass ? (double)before < target && (double)(before + step) >= target : before < want && before + step >= want;
@@ -308,10 +313,12 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     // other's latency.)
     const int lane = tid & 31, run4 = ((n / 4 + threads / 32 - 1) / (threads / 32) + 31) & ~31, first4 = (tid >> 5) * run4;      // in fours
     auto fours = [&](auto f) {
+#pragma unroll 1
         for (int i = lane; i < run4; i += 32)
             f(first4 + i < n / 4 ? *reinterpret_cast<const float4*>(x_s + 4 * (first4 + i)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY));
     };
     auto each_token = [&](auto f) {
+#pragma unroll 1
         for (int j = tid; j < n / 4; j += threads) {
             const float4 x = *reinterpret_cast<const float4*>(x_s + 4 * j);
             f(x.x);
@@ -568,6 +575,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             const int per = (run4 * 4 + threads - 1) / threads, begin = run * run4 * 4 + tid * per, stop = min(n, min(begin + per, (run + 1) * run4 * 4));
             u64 mine = 0, all;
             uint32_t my_ties = 0, all_run_ties;
+#pragma unroll 1
             for (int j = begin; j < stop; ++j) {
                 u64 m;
                 const int s = kept_side(x_s[j], &m);
@@ -577,7 +585,8 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             u64 at = cta_before + run_sum_s[run] + block_exclusive_scan<u64>(mine, scan64_s, &all);
             uint32_t tie_at = cta_ties_before + run_ties_s[run] + block_exclusive_scan<uint32_t>(my_ties, scan32_s, &all_run_ties);
             if (running(at, tie_at) <= target && target < running(at + mine, tie_at + my_ties)) {
-                for (int j = begin; j < stop; ++j) {
+    #pragma unroll 1
+            for (int j = begin; j < stop; ++j) {
                     u64 m;
                     const int s = kept_side(x_s[j], &m);
                     at += s > 0 ? m : 0;
@@ -644,7 +653,7 @@ extern "C" onela_status onela_sample_tokens(const onela_sample_args* g, void* st
     static_assert(MAX_VOCAB / 8 + 32 <= MAX_SLICE, "a slice with its row's odd start and end");
     if (g->vocab > MAX_VOCAB || g->rows > 0x7fffffff / MAX_CLUSTER) return ONELA_E_CAPACITY;
     if (g->rows == 0) return ONELA_OK;
-    if (!g->logits_dev || !g->uniforms_dev || !g->tokens_out_dev || g->logits_stride < g->vocab) return ONELA_E_INVAL;
+    if (!g->logits_dev || !g->uniforms_dev || !g->tokens_out_dev || (g->logits_stride != 0 && g->logits_stride < g->vocab)) return ONELA_E_INVAL;
     if (reinterpret_cast<uintptr_t>(g->logits_dev) % (g->dtype == ONELA_DTYPE_BF16 ? 2 : 4) != 0) return ONELA_E_INVAL;
     int log_vocab = 0;
     while ((1ll << log_vocab) < g->vocab) ++log_vocab;

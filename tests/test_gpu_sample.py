@@ -150,6 +150,14 @@ def test_strided_rows_streams_and_graphs():
     assert np.array_equal(tok.cpu().numpy(), _sample(x, u)[0])
 
 
+def test_many_draws_from_one_row():
+    """A row that is expanded over the draws (stride 0)."""
+    x, _ = _logits(1, 3001, 21)
+    u = torch.rand((7,), generator=torch.Generator(device="cuda").manual_seed(22), device="cuda")
+    a, b = _sample(x.expand(7, 3001), u, top_k=50), _sample(x.expand(7, 3001).contiguous(), u, top_k=50)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
 def test_results_do_not_depend_on_the_rest_of_the_batch():
     x, u = _logits(150, 20011, 14)
     all_rows = _sample(x, u, top_p=0.9)
