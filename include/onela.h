@@ -281,8 +281,8 @@ int32_t onela_uses_tensor_core_path(const onela_ctx* ctx);
  * Element pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when interleaved, i < rotary_dim / 2, turn by the angle
  * position * inv_freq[i]: (a, b) -> (a cos - b sin, b cos + a sin).  Angles are formed in 64 bits and any int32 position is
  * fine, negative ones included.  Queries are multiplied by q_scale at the end.  Norms and products in fp32, one rounding.
- * q_out may be q and k_out may be k with the same stride (in place); otherwise outputs overlap nothing.  More than 2^31 - 1 tokens or 2^30 - 1
- * elements in a token's heads: ONELA_E_CAPACITY. */
+ * q_out may be q and k_out may be k with the same stride (in place); otherwise outputs overlap nothing.  More than 2^31 - 1 tokens or 2^20
+ * heads of queries or of keys: ONELA_E_CAPACITY. */
 typedef struct onela_norm_rotate_args {
     const void *q_dev, *k_dev;        /* [n_tokens][num_q_heads][head_dim], [n_tokens][num_k_heads][head_dim] in dtype */
     void *q_out_dev, *k_out_dev;      /* the same shapes and dtype */
@@ -317,7 +317,7 @@ onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream)
  * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it
  * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores.
  * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED.
- * At most 65 535 sequences and 2^31 - 256 tokens, else ONELA_E_CAPACITY. */
+ * At most 65 535 sequences, 65 535 value heads and 2^31 - 256 tokens, else ONELA_E_CAPACITY. */
 typedef struct onela_delta_rule_args {
     const void *q_dev, *k_dev, *v_dev;       /* [n_tokens][num_heads][dk] twice, [n_tokens][num_v_heads][dv] in dtype */
     const float *alpha_dev, *beta_dev;       /* [n_tokens][num_v_heads] */

@@ -50,20 +50,30 @@ class OnelaConfig(ctypes.Structure):
         return self.num_v_heads or self.num_heads
 
 
-class NormRotateArgs(ctypes.Structure):
+class _Args(ctypes.Structure):
+    """Keyword arguments only; a size that 32 bits do not hold is refused, where ctypes would cut it off."""
+
+    def __init__(self, **fields):
+        for name, kind in self._fields_:
+            if kind is c_int32 and not -2 ** 31 <= fields.get(name, 0) < 2 ** 31:
+                raise OnelaError(E_CAPACITY, f"{name} = {fields[name]}")
+        super().__init__(**fields)
+
+
+class NormRotateArgs(_Args):
     _fields_ = [(n, c_void_p) for n in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "positions", "inv_freq")] + \
                [(n, c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride", "n_tokens")] + \
                [(n, c_int32) for n in ("num_q_heads", "num_k_heads", "head_dim", "rotary_dim", "interleaved", "norm", "dtype")] + \
                [("eps", c_float), ("q_scale", c_float)]
 
 
-class DeltaRuleArgs(ctypes.Structure):
+class DeltaRuleArgs(_Args):
     _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "alpha", "beta", "states", "out", "starts", "slots", "fresh", "status")] + \
                [(n, c_int64) for n in ("q_stride", "k_stride", "v_stride", "out_stride", "gate_stride", "state_stride", "n_tokens")] + \
                [(n, c_int32) for n in ("num_sequences", "num_states", "max_tokens", "num_heads", "num_v_heads", "dk", "dv", "dtype")]
 
 
-class SampleArgs(ctypes.Structure):
+class SampleArgs(_Args):
     _fields_ = [(n, c_void_p) for n in ("logits", "uniforms", "temperature", "top_p", "min_p", "top_k", "tokens_out", "logprobs_out")] + \
                [("logits_stride", c_int64)] + [(n, c_int32) for n in ("rows", "vocab", "dtype")]
 

@@ -178,10 +178,10 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
     if (!g) return ONELA_E_INVAL;
     if (g->dtype != ONELA_DTYPE_F32 && g->dtype != ONELA_DTYPE_BF16) return ONELA_E_INVAL;
     if (g->n_tokens < 0 || g->num_sequences < 0 || g->num_states < 0 || g->max_tokens < 0 || g->num_heads < 1 || g->num_v_heads < 1) return ONELA_E_INVAL;
-    if (g->num_v_heads % g->num_heads != 0 || g->num_v_heads > 65535) return ONELA_E_INVAL;
+    if (g->num_v_heads % g->num_heads != 0) return ONELA_E_INVAL;
     if (g->dk != 32 && g->dk != 64 && g->dk != 128 && g->dk != 256) return ONELA_E_UNSUPPORTED;
     if (g->dv < 32 || g->dv % 32 != 0 || g->dv > 512) return ONELA_E_UNSUPPORTED;
-    if (g->num_sequences > 65535 || g->n_tokens > 0x7fffff00ll) return ONELA_E_CAPACITY;
+    if (g->num_sequences > 65535 || g->num_v_heads > 65535 || g->n_tokens > 0x7fffff00ll) return ONELA_E_CAPACITY;
     if (!g->starts_dev && g->n_tokens != g->num_sequences) return ONELA_E_INVAL;
     if (!g->slots_dev && g->num_states < g->num_sequences) return ONELA_E_INVAL;
     if (g->num_sequences == 0) return ONELA_OK;

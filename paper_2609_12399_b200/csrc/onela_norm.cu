@@ -244,14 +244,13 @@ extern "C" onela_status onela_norm_rotate(const onela_norm_rotate_args* g, void*
     if (g->norm != ONELA_NORM_NONE && g->norm != ONELA_NORM_L2 && g->norm != ONELA_NORM_RMS) return ONELA_E_INVAL;
     const long long es = g->dtype == ONELA_DTYPE_BF16 ? 2 : 4;
     constexpr int32_t MAX_HEADS = 1 << 20;
-    if (g->n_tokens < 0 || g->num_q_heads < 0 || g->num_k_heads < 0 || g->num_q_heads > MAX_HEADS || g->num_k_heads > MAX_HEADS || g->head_dim < 1) return ONELA_E_INVAL;
+    if (g->n_tokens < 0 || g->num_q_heads < 0 || g->num_k_heads < 0 || g->head_dim < 1) return ONELA_E_INVAL;
     if (g->head_dim % 8 != 0 || g->head_dim > 256) return ONELA_E_UNSUPPORTED;
     if (g->rotary_dim < 0 || g->rotary_dim > g->head_dim) return ONELA_E_INVAL;
     if (g->rotary_dim % 16 != 0) return ONELA_E_UNSUPPORTED;
     if (!(g->eps >= 0.f)) return ONELA_E_INVAL;
-    if (g->n_tokens == 0 || g->num_q_heads + g->num_k_heads == 0) return ONELA_OK;
-    const long long heads = (long long)g->num_q_heads + g->num_k_heads;
-    if (g->n_tokens > 0x7fffffffll || heads * g->head_dim > 0x3fffffffll) return ONELA_E_CAPACITY;      // CTAs of one launch, 32-bit offsets within a token
+    if (g->n_tokens == 0 || (g->num_q_heads == 0 && g->num_k_heads == 0)) return ONELA_OK;
+    if (g->n_tokens > 0x7fffffffll || g->num_q_heads > MAX_HEADS || g->num_k_heads > MAX_HEADS) return ONELA_E_CAPACITY;      // CTAs of one launch, 32-bit offsets within a token
     if (g->rotary_dim > 0 && (!g->positions_dev || !g->inv_freq_dev)) return ONELA_E_INVAL;
     if (!aligned16(g->q_weight_dev) || !aligned16(g->k_weight_dev)) return ONELA_E_INVAL;
     const Rows set[4] = {{static_cast<const char*>(g->q_dev), g->q_stride * es, (long long)g->num_q_heads * g->head_dim * es, g->n_tokens},

@@ -585,8 +585,8 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
             u64 at = cta_before + run_sum_s[run] + block_exclusive_scan<u64>(mine, scan64_s, &all);
             uint32_t tie_at = cta_ties_before + run_ties_s[run] + block_exclusive_scan<uint32_t>(my_ties, scan32_s, &all_run_ties);
             if (running(at, tie_at) <= target && target < running(at + mine, tie_at + my_ties)) {
-    #pragma unroll 1
-            for (int j = begin; j < stop; ++j) {
+#pragma unroll 1
+                for (int j = begin; j < stop; ++j) {
                     u64 m;
                     const int s = kept_side(x_s[j], &m);
                     at += s > 0 ? m : 0;

@@ -43,6 +43,7 @@ def _sample(**kw):
     (dict(q_out=A + 16), binding.E_INVAL), (dict(k_out=A), binding.E_INVAL), (dict(q_out=2 * A - 1024), binding.E_INVAL), (dict(k_out=3 * A + 1024), binding.E_INVAL),
     (dict(q=A, q_stride=1024, q_out=A, q_out_stride=512), binding.E_INVAL),
     (dict(q_stride=1 << 50), binding.E_INVAL), (dict(n_tokens=1 << 45), binding.E_CAPACITY),
+    (dict(num_q_heads=(1 << 20) + 1, q_stride=1 << 28), binding.E_CAPACITY), (dict(num_k_heads=(1 << 31) - 1), binding.E_CAPACITY),
     (dict(n_tokens=0), 0), (dict(num_q_heads=0, num_k_heads=0), 0),
 ])
 def test_norm_rotate(lib, kw, status):
@@ -56,7 +57,7 @@ def test_norm_rotate(lib, kw, status):
     (dict(dk=512), binding.E_UNSUPPORTED), (dict(dv=48), binding.E_UNSUPPORTED), (dict(dv=544), binding.E_UNSUPPORTED), (dict(dv=0), binding.E_UNSUPPORTED),
     (dict(dtype=7), binding.E_INVAL), (dict(n_tokens=-1), binding.E_INVAL), (dict(num_sequences=-1), binding.E_INVAL), (dict(max_tokens=-1), binding.E_INVAL),
     (dict(starts=0), binding.E_INVAL), (dict(slots=0, num_states=2), binding.E_INVAL), (dict(num_sequences=70000), binding.E_CAPACITY),
-    (dict(n_tokens=1 << 31), binding.E_CAPACITY), (dict(num_sequences=0), 0),
+    (dict(n_tokens=1 << 31), binding.E_CAPACITY), (dict(num_v_heads=65536), binding.E_CAPACITY), (dict(num_sequences=0), 0),
     # outputs and states over inputs and over one another
     (dict(out=A), binding.E_INVAL), (dict(out=3 * A), binding.E_INVAL), (dict(out=2 * A + 256, out_stride=768), binding.E_INVAL), (dict(states=3 * A + 512), binding.E_INVAL),
     (dict(states=7 * A), binding.E_INVAL),
@@ -72,6 +73,15 @@ def test_delta_rule(lib, kw, status):
 ])
 def test_sample_tokens(lib, kw, status):
     assert lib.onela_sample_tokens(ctypes.byref(_sample(**kw)), None) == status
+
+
+@pytest.mark.parametrize("make,field", [(_norm, "num_q_heads"), (_norm, "rotary_dim"), (_delta, "num_sequences"), (_delta, "max_tokens"), (_sample, "vocab"), (_sample, "rows")])
+def test_sizes_beyond_32_bits(make, field):
+    """Cut off to 32 bits they would be small and pass."""
+    make(**{field: 2 ** 31 - 1})
+    for n in (2 ** 31, 2 ** 32 + 1, -2 ** 31 - 1):
+        with pytest.raises(P.OnelaError, match=field):
+            make(**{field: n})
 
 
 def test_null_arguments(lib):
