@@ -25,9 +25,11 @@
 // segment from its state.  The state before a segment, its predecessor's B before that, and M lie meanwhile in the segment's own rows of the caller's `out`, which OUTPUTS overwrites when it
 // has read them: a segment holds enough tokens for that, or its sequence is not cut.
 //
-// Precision.  S, X, D and the results are fp32; operands are sums of two fp16 numbers (22 to 23 significant bits) but for keys and queries
-// in bf16, which one fp16 number holds exactly, and for what only bf16 outputs see (S and D in their products with the queries' side, P): one fp16 number,
-// 2^-12 relative, a sixteenth of the outputs' own rounding.  Every operand row has its own power of two.
+// Precision.  S, X, D and the results are fp32.  Where a product runs over the state's columns (S [K; Q]^T, [K; Q] K^T) or into them (D K) an operand's row has one size
+// and its own power of two: operands are sums of two fp16 numbers (22 to 23 significant bits), keys and queries in bf16 one, exact; S in its product with bf16 queries
+// one as well (2^-11).  Along the tokens (T, P, X, D) sizes differ by what the gates have left, by far more than fp16's range: those operands are sums of three bf16 numbers (24 bits,
+// fp32's range), with nothing to scale.  So what fades, or comes under a small key, keeps its places; only below 2^-110 they go.  (Two fp16 numbers with a scale per
+// row instead: outputs and states wrong in the third digit behind 64 gates of 0.8, in the first behind 64 of 0.6.)
 //
 // What bounds it: a chunk takes a CTA 11 000 cycles (5.9 us), of which the chain of its products and their operands is the critical path, and 24 000 warp
 // instructions (issue slots 56 % used; the preparation 8 500 of them, the chain twelve, the outputs three thousand).  With both SMs of a pair at work it was 8.4 us,
@@ -64,30 +66,37 @@ using sm100::umma_desc;
 
 constexpr int ROWS = 128;                 // state rows per CTA
 constexpr int KQ_BLOCK = 2 * TILE;        // 128 rows (64 of K, 64 of Q) of 64 fp16
-constexpr int NARROW = 3, WIDE = 12;      // largest elements of operand rows: K, Q, T, P in [2^3, 2^4), S, X, D in [2^12, 2^13)
+constexpr int NARROW = 3, WIDE = 12;      // largest elements of fp16 operand rows: K, Q in [2^3, 2^4), S and the state's D in [2^12, 2^13)
+// T and P are lower triangular, so the columns of a K step (16 tokens) are kept from their first row on: 64, 48, 32 and 16 rows, a step's two halves
+// (8 columns, 16 bytes a row) one after the other; three bf16 parts.
+constexpr int TRI = (64 + 48 + 32 + 16) * 32, TRI_BYTES = 3 * TRI;
+__host__ __device__ constexpr int tri_at(int step) { return step * 2048 - step * (step - 1) * 256; }
 constexpr int CHAIN_BARRIER = 3, OUT_BARRIER = 4;      // named barriers (1, 2: the preparing teams')
 
 template <int D, typename T>
 struct Shape {
     static constexpr bool WIDE_T = sizeof(T) == 4;
     static constexpr int KB = D > 64 ? D / 64 : 1;                 // K blocks of 64 elements
-    static constexpr int PARTS = WIDE_T ? 2 : 1;                   // fp16 parts of a key, a query, P
+    static constexpr int PARTS = WIDE_T ? 2 : 1;                   // fp16 parts of a key, a query
     static constexpr int PREPS = WIDE_T && D == 128 ? 1 : 2;       // preparing teams
-    static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = 2;
+    static constexpr int K_STAGES = WIDE_T && D == 128 ? 2 : 3, T_STAGES = !WIDE_T && D == 128 ? 1 : 2, P_STAGES = 2;
     static constexpr int PREP_THREADS = 128 * PREPS, GROUPS = D == 64 ? 4 : 2, CHAIN_THREADS = 128 * GROUPS, THREADS = PREP_THREADS + CHAIN_THREADS + 128;
-    static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK, T_BYTES = 2 * TILE, P_BYTES = PARTS * TILE;
+    static constexpr int KQ_BYTES = PARTS * KB * KQ_BLOCK;
     static constexpr bool STAGE_V = !WIDE_T;                       // values through shared memory (fp32: there is no room)
     static constexpr int V_BYTES = STAGE_V ? C * ROWS * (int)sizeof(T) : 0;
     static constexpr int O_TOKENS = 32, O_BYTES = WIDE_T ? 0 : O_TOKENS * ROWS * 2;      // outputs on their way out (bf16)
     static constexpr int A_BYTES = (C * AP * 4 + 1023) / 1024 * 1024, X_BYTES = 5 * 1024;
-    // per K stage: beta g / key scale, g / query scale, beta, g_C; per T stage: weights of D's columns for the state, what undoes P's rows' scales
-    // and T's
-    static constexpr int KCO = 3 * C + 4, TCO = 2 * C + 4;
-    static constexpr int SMALL = (K_STAGES * KCO + T_STAGES * TCO + PREPS * (128 + 3 * C) + (2 * GROUPS + 4) * ROWS) * 4 + 256;
-    static constexpr int SMEM = K_STAGES * KQ_BYTES + T_STAGES * (T_BYTES + P_BYTES) + V_BYTES + O_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
+    // per K stage: beta g / key scale, g / query scale, beta, g_C; per P stage: weights of D's columns for the state
+    static constexpr int KCO = 3 * C + 4, TCO = C;
+    static constexpr int SMALL = (K_STAGES * KCO + P_STAGES * TCO + PREPS * (128 + 3 * C) + (2 * GROUPS + 2) * ROWS) * 4 + 256;
+    static constexpr int SMEM = K_STAGES * KQ_BYTES + (T_STAGES + P_STAGES) * TRI_BYTES + V_BYTES + O_BYTES + PREPS * (A_BYTES + X_BYTES) + SMALL + 1024;
     static_assert(SMEM <= 232448, "shared memory");
-    // tensor memory: S operand / D K | Z, X operand, D operand for the outputs (64) ; S Q^T (64) | D (64) | D P^T (64) | per preparing team 64
-    static constexpr uint32_t Z_COL = 128, O1_COL = Z_COL + C, D_COL = 256, O2_COL = 320, PREP_COL = 384, TMEM_COLS = 512;
+    // tensor memory: S operand, then X operand (96), then D K | D operand for the outputs (96), in its last 64 Z before that | S Q^T (64) | D, then its operand for
+    // the state (64) | D P^T (64) | [K; Q] K^T of the preparing teams (64 each; one for both where D K takes 128)
+    static constexpr int X_STEP = 24;                              // columns of a K step in three bf16 parts
+    static constexpr uint32_t DO_COL = D > 96 ? D : 96, Z_COL = DO_COL + 32, O1_COL = Z_COL + C, D_COL = O1_COL + C, O2_COL = D_COL + C, PREP_COL = O2_COL + C, TMEM_COLS = 512;
+    static constexpr bool ONE_ACC = PREPS == 2 && D == 128;
+    static_assert(PREP_COL + (ONE_ACC ? 1 : PREPS) * C <= TMEM_COLS, "tensor memory");
     // registers: 640 threads start with 96 each; at dk = 128 the chain's state rows take what the other roles leave
     static constexpr bool SPLIT_REGS = THREADS == 640 && D == 128;
     static constexpr int PREP_REGS = 72, CHAIN_REGS = 128, OUT_REGS = 80;
@@ -104,6 +113,38 @@ __device__ __forceinline__ float2 pair(float x, float y) { return make_float2(x,
 __device__ __forceinline__ float2 pair(uint32_t x, uint32_t y) { return make_float2(__uint_as_float(x), __uint_as_float(y)); }
 // (the compiler keeps what it knows to be the same in all lanes where the MMAs want it)
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// Descriptor of a K step of T or P (tri_desc of the tile plus tri_step): K-major without a swizzle, groups of eight rows 128 bytes apart, the halves as far
+// as the step has rows.
+__device__ __forceinline__ uint64_t tri_desc(uint32_t smem_addr) { return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46); }
+__host__ __device__ constexpr uint64_t tri_step(int step) { return (uint64_t)(tri_at(step) >> 4) | ((uint64_t)(C - 16 * step) << 16); }
+// Eight numbers of row `row` (fp32 bits), half `half` of K step `step`, as three bf16 parts.
+__device__ __forceinline__ void store_tri(uint8_t* tile, int row, int step, int half, const uint32_t* x) {
+    uint32_t part[3][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t w[3];
+        split_bf16(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]), w);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) part[p][e] = w[p];
+    }
+    uint8_t* to = tile + tri_at(step) + (half * (C - 16 * step) + row - 16 * step) * 16;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(to + p * TRI) = make_uint4(part[p][0], part[p][1], part[p][2], part[p][3]);
+}
+// Sixteen numbers as a K step of a tensor-memory operand in three bf16 parts, eight columns each.
+__device__ __forceinline__ void triple_to_tmem(uint32_t taddr, const float* x) {
+    uint32_t w[24];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint32_t part[3];
+        split_bf16(x[2 * e], x[2 * e + 1], part);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) w[8 * p + e] = part[p];
+    }
+    tmem_st16(taddr, w);
+    tmem_st8(taddr + 16, w + 16);
+}
 
 enum { WHOLE, MAPS, OUTPUTS };
 
@@ -135,29 +176,31 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* t_ring = smem + Z::K_STAGES * Z::KQ_BYTES;
-    uint8_t* p_ring = t_ring + Z::T_STAGES * Z::T_BYTES;
-    uint8_t* prep_s = p_ring + Z::T_STAGES * Z::P_BYTES;                            // per preparing team: matrix, scratch
+    uint8_t* p_ring = t_ring + Z::T_STAGES * TRI_BYTES;
+    uint8_t* prep_s = p_ring + Z::P_STAGES * TRI_BYTES;                             // per preparing team: matrix, scratch
     T* v_s = reinterpret_cast<T*>(prep_s + Z::PREPS * (Z::A_BYTES + Z::X_BYTES));   // [token][row]
     uint16_t* o_s = reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(v_s) + Z::V_BYTES);       // [token][row]
     float* kco_s = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(o_s) + Z::O_BYTES);
     float* tco_s = kco_s + Z::K_STAGES * Z::KCO;
-    float* tok_s = tco_s + Z::T_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
-    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [2][GROUPS][ROWS] largest of a row's part: S, X, D in turn; D as weighted
-    float* inv_s = max_s + 2 * Z::GROUPS * ROWS;                                                // [2][2][ROWS] what undoes the scales of S and D rows
-    uint64_t* bars = reinterpret_cast<uint64_t*>(inv_s + 4 * ROWS);
+    float* tok_s = tco_s + Z::P_STAGES * Z::TCO;                                    // per preparing team: what undoes the tile rows' scales [128], alpha, g_C / g, beta
+    float* max_s = tok_s + Z::PREPS * (128 + 3 * C);                                // [2][GROUPS][ROWS] largest of a row's part: S; D as weighted
+    float* inv_s = max_s + 2 * Z::GROUPS * ROWS;                                    // [2][ROWS] what undoes the scales of S rows
+    uint64_t* bars = reinterpret_cast<uint64_t*>(inv_s + 2 * ROWS);
     auto bar_k = [&](int i) { return smem_u32(bars + i % Z::K_STAGES); };           // keys, queries, their weights
     auto bar_kfree = [&](int i) { return smem_u32(bars + 3 + i % Z::K_STAGES); };
     // T and P: the barriers of even and odd chunks, however many tiles there are (a wait by parity does not tell a chunk's turn from the
     // one after next, and a team that comes early would take the one before for its own)
     auto bar_t = [&](int i) { return smem_u32(bars + 6 + (i & 1)); };
-    auto bar_tfree = [&](int i) { return smem_u32(bars + 8 + (i & 1)); };
+    auto bar_tfree = [&](int i) { return smem_u32(bars + 8 + (i & 1)); };           // T read, P read
+    auto bar_pfree = [&](int i) { return smem_u32(bars + 19 + (i & 1)); };
     auto k_turn = [](int i) { return (uint32_t)(i / Z::K_STAGES) & 1; };
     auto t_turn = [](int i) { return (uint32_t)(i >> 1) & 1; };
     const uint32_t bar_v = smem_u32(bars + 10), bar_vfree = smem_u32(bars + 11);    // values
     const uint32_t bar_z = smem_u32(bars + 12), bar_d = smem_u32(bars + 13), bar_s = smem_u32(bars + 14), bar_o = smem_u32(bars + 15);      // MMA sets
     const uint32_t bar_ofree = smem_u32(bars + 16);                                 // the outputs' accumulators read out
     auto bar_prep = [&](int w) { return smem_u32(bars + 17 + w); };
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+    const uint32_t bar_acc = smem_u32(bars + 21);                                   // a team has read its products out (ONE_ACC)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -184,8 +227,10 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(bars + 6 + s), 128);
-            mbar_init(smem_u32(bars + 8 + s), 1 + 128);
+            mbar_init(smem_u32(bars + 8 + s), 1);
+            mbar_init(smem_u32(bars + 19 + s), 1);
         }
+        mbar_init(bar_acc, 128);
         mbar_init(bar_v, 128);
         mbar_init(bar_vfree, 1);
         mbar_init(bar_z, 1);
@@ -234,7 +279,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         float* X_s = A_s + Z::A_BYTES / 4;                                                      // [32][36]
         float* scale_s = tok_s + team * (128 + 3 * C);
         float *alpha_s = scale_s + 128, *behind_s = alpha_s + C, *total_s = behind_s + C;       // total_s: product of the gates of either warp
-        const uint32_t acc_at = uniform(tmem_base + Z::PREP_COL + team * C);
+        const uint32_t acc_at = uniform(tmem_base + Z::PREP_COL + (Z::ONE_ACC ? 0 : team * C));
         constexpr int VEC = Vec16<T>::N, CPR = D / VEC, LR = CPR < 8 ? CPR : 8;      // 16-byte chunks and lanes per row
         constexpr int PASS_ROWS = 128 / LR, PASSES = 128 / PASS_ROWS, NC = CPR / LR;
         constexpr int BATCH = PASSES * NC > 4 ? 4 / NC : PASSES;                     // passes whose loads are in flight together
@@ -246,6 +291,12 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             alpha_next = gate_of(a.alpha, team * C + pt, 1.f);
             beta_next = gate_of(a.beta, team * C + pt, 0.f);
         }
+        auto products_read = [&] {                                                  // (their place is the other team's next)
+            if (Z::ONE_ACC) {
+                tc_fence_before();
+                arrive(bar_acc);
+            }
+        };
         uint32_t phase = 0;
         for (int i = team; i < n; i += Z::PREPS) {
             const int t0 = i * C;
@@ -320,6 +371,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     beta_next = gate_of(a.beta, t0 + Z::PREPS * C + pt, 0.f);
                 }
             }
+            if (Z::ONE_ACC && i > 0) wait(bar_acc, (i - 1) & 1);
             proxy_fence();
             tc_fence_before();
             if (bar_or(1 + team, 128, fail ? 1 : 0)) { fail = true; break; }
@@ -359,8 +411,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             phase ^= 1;
             tc_fence_after();
             // A's row i by thread i, P's row i by thread 64 + i.  (g_i / g_l) runs from the right: the product of the gates behind l.
-            uint8_t *T_s = t_ring + i % Z::T_STAGES * Z::T_BYTES, *P_s = p_ring + i % Z::T_STAGES * Z::P_BYTES;
-            float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
+            uint8_t *T_s = t_ring + i % Z::T_STAGES * TRI_BYTES, *P_s = p_ring + i % Z::P_STAGES * TRI_BYTES;
+            float* tco = tco_s + i % Z::P_STAGES * Z::TCO;
             if (w4 < 2) {
                 const float coef = beta * scale_s[pt];
                 float ratio = 1.f;
@@ -383,6 +435,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                         *reinterpret_cast<float4*>(A_s + pt * AP + cb * 16 + e) = make_float4(row[0], row[1], row[2], row[3]);
                     }
                 }
+                products_read();
                 __syncwarp();
                 // T = (I + A)^-1 in place, from the diagonal out.  Blocks of 16, two per warp, one column per lane by forward
                 // substitution; then a warp's two blocks are joined, then the two warps': - T22 A21 T11 below the diagonal.
@@ -417,25 +470,13 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
                 for (int r = 0; r < 8; ++r) B21[r * AP + col] = -acc[r];
             } else {
-                // P's scale is a bound's, so that one round does: a row's scaled dot products are below 2^15 (128 x 2^4 x 2^4), the keys' scales
-                // are taken relative to the coarsest key's, and gates beyond 1 multiply to `up` at the most
                 const int me = pt - C;
-                float coarsest = fmaxf(scale_s[lane], scale_s[lane + 32]), up = fmaxf(alpha_s[lane], 1.f) * fmaxf(alpha_s[lane + 32], 1.f);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    coarsest = fmaxf(coarsest, __shfl_xor_sync(0xffffffffu, coarsest, o));
-                    up *= __shfl_xor_sync(0xffffffffu, up, o);
-                }
-                float down, up2, undo, relative;
-                pow2_scale(up, -1, down, up2);                                  // up times down in [1 / 2, 1)
-                pow2_scale(coarsest, 0, relative, undo);                        // (a power of two: relative = 1 / coarsest)
-                const float sc = 0.25f * down;
+                const float query = scale_s[pt];
                 float ratio = 1.f;
-                if (i >= Z::T_STAGES) wait(bar_tfree(i - Z::T_STAGES), t_turn(i - Z::T_STAGES));
-                tco[C + me] = (4.f * up2) * (scale_s[pt] * undo);
+                if (i >= Z::P_STAGES) wait(bar_pfree(i - Z::P_STAGES), t_turn(i - Z::P_STAGES));
 #pragma unroll 1
                 for (int cb = 3; cb >= 0; --cb) {
-                    uint32_t v[16], hi[8], lo[8];
+                    uint32_t v[16];
                     tmem_ld16(acc_at + cb * 16 + ((uint32_t)(w4 * 32) << 16), v);
                     tc_wait_ld();
 #pragma unroll
@@ -445,23 +486,17 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
 #pragma unroll
                         for (int f = 3; f >= 0; --f) {
                             const int l = cb * 16 + e + f;
-                            const float x = __uint_as_float(v[e + f]) * (kiv[f] * relative);
-                            v[e + f] = __float_as_uint(l <= me ? (ratio * sc) * x : 0.f);
+                            const float x = (__uint_as_float(v[e + f]) * kiv[f]) * query;
+                            v[e + f] = __float_as_uint(l <= me ? ratio * x : 0.f);
                             ratio *= l <= me ? alv[f] : 1.f;
                         }
                     }
+                    if (me >= 16 * cb) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if constexpr (PARTS > 1) split2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]), hi[e], lo[e]);
-                        else hi[e] = pack_f16x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint8_t* dst = P_s + me * 128 + (((2 * cb + e) ^ (me & 7)) << 4);
-                        *reinterpret_cast<uint4*>(dst) = make_uint4(hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-                        if constexpr (PARTS > 1) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
+                        for (int e = 0; e < 2; ++e) store_tri(P_s, me, cb, e, v + 8 * e);
                     }
                 }
+                products_read();
             }
             tc_fence_before();
             bar_or(1 + team, 128, 0);
@@ -477,36 +512,20 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             }
             if (i >= Z::T_STAGES) wait(bar_tfree(i - Z::T_STAGES), t_turn(i - Z::T_STAGES));
             if (bar_or(1 + team, 128, fail ? 1 : 0)) { fail = true; break; }
-            // T as an operand tile (fp16 hi, lo): row pt / 2 by threads pt and pt + 1, columns 16 h .. and 32 + 16 h .. (conflict-free reads)
+            // T as an operand tile: row pt / 2 by threads pt and pt + 1, columns 16 h .. and 32 + 16 h .. (conflict-free reads).  (What lies above the
+            // diagonal is zero, A's there too.)
             {
                 const int ti = pt >> 1, hf = pt & 1;
-                float t[32], m = 0.f;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float4 x = *reinterpret_cast<const float4*>(A_s + ti * AP + 16 * hf + (q >> 2) * 32 + (q & 3) * 4);
-                    t[4 * q] = x.x; t[4 * q + 1] = x.y; t[4 * q + 2] = x.z; t[4 * q + 3] = x.w;
-                }
-                // (what lies above the diagonal is zero, A's there too; one scale for the tile, whose diagonal is 1)
-#pragma unroll
-                for (int q = 0; q < 32; q += 2) m = max3(m, t[q], t[q + 1]);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                if (lane == 0) X_s[w4] = m;
-                bar_or(1 + team, 128, 0);
-                m = fmaxf(fmaxf(X_s[0], X_s[1]), fmaxf(X_s[2], X_s[3]));
-                float sc, inv;
-                pow2_scale(m, NARROW, sc, inv);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {                               // chunks of eight columns
-                    const int ch = 4 * (c >> 1) + 2 * hf + (c & 1), at = ti * 128 + ((ch ^ (ti & 7)) << 4);
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split2(t[8 * c + 2 * e] * sc, t[8 * c + 2 * e + 1] * sc, hi[e], lo[e]);
-                    *reinterpret_cast<uint4*>(T_s + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4*>(T_s + TILE + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    const int step = 2 * (c >> 1) + hf, half = c & 1;
+                    if (ti < 16 * step) continue;
+                    const float4 x = *reinterpret_cast<const float4*>(A_s + ti * AP + 16 * step + 8 * half), y = *reinterpret_cast<const float4*>(A_s + ti * AP + 16 * step + 8 * half + 4);
+                    const uint32_t t[8] = {__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z), __float_as_uint(x.w),
+                                           __float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
+                    store_tri(T_s, ti, step, half, t);
                 }
                 if (hf == 0) tco[ti] = behind_s[ti];
-                if (pt == 0) tco[2 * C] = inv;
             }
             proxy_fence();
             arrive(bar_t(i));
@@ -519,8 +538,9 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         const bool is_row = identity ? r < D : row_base + r < a.dv;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem_base + lanes + c * H, z_at = tmem_base + lanes + Z::Z_COL + TG * c, d_at = tmem_base + lanes + Z::D_COL + TG * c;
+        const uint32_t x_at = tmem_base + lanes + TB * c * Z::X_STEP, do_at = x_at + Z::DO_COL;
         const bool issuer = warp == 4 * Z::PREPS, leader = issuer && lane == 0;
-        // largest magnitudes (kind 0: S, X, D in turn, barriers between them; 1: D as weighted): mine, and of the whole row when all have met
+        // largest magnitudes (kind 0: S; 1: D as weighted): mine, and of the whole row when all have met
         float* mine = max_s + c * ROWS + r;
         auto of_row = [&](int kind) {
             const float* m = max_s + kind * G * ROWS + r;
@@ -560,16 +580,15 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         for (int i = 0; i < n; ++i) {
             const uint32_t turn = i & 1;
             const float* kco = kco_s + i % Z::K_STAGES * Z::KCO;
-            const float* tco = tco_s + i % Z::T_STAGES * Z::TCO;
-            float sc;
+            const float* tco = tco_s + i % Z::P_STAGES * Z::TCO;
             // ---- Z = S K^T, and S Q^T ----
             m = of_row(0);
-            if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f && scale_row < 0x1p60f)) {
-                float inv;
+            if (!(m < 0x1p15f) || (m < 0x1p6f && m > 0.f && scale_row < 0x1p110f)) {
+                float sc, inv;
                 pow2_scale(m, WIDE, sc, inv);
-                if (sc > 0x1p60f) {                               // (2^-e stays a normal number: a state below 2^-114 loses places, as it would in fp32)
-                    sc = 0x1p60f;
-                    inv = 0x1p-60f;
+                if (sc > 0x1p110f * inv_row) {                    // (what undoes it, in products with D too, stays a normal number: a state below 2^-110 loses places)
+                    sc = 0x1p110f * inv_row;
+                    inv = 0x1p-110f * scale_row;
                 }
 #pragma unroll
                 for (int e = 0; e < H; e += 2) {
@@ -624,8 +643,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             }
             wait_mma(bar_z, turn);
             tc_fence_after();
-            // ---- X = (V^T - Z diag(g)) diag(beta) ----
-            float x[TG], mx = 0.f;
+            // ---- X = (V^T - Z diag(g)) diag(beta), over the S operand (read by now) ----
+            float x[TG];
             const float2 neg = pair(-inv_row, -inv_row);
 #pragma unroll
             for (int b = 0; b < TB; ++b) {
@@ -644,36 +663,37 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     const float2 y0 = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), neg), pair(gz.x, gz.y), __fmul2_rn(pair(u[e], u[e + 1]), pair(be.x, be.y)));
                     const float2 y1 = __ffma2_rn(__fmul2_rn(pair(v[e + 2], v[e + 3]), neg), pair(gz.z, gz.w), __fmul2_rn(pair(u[e + 2], u[e + 3]), pair(be.z, be.w)));
                     x[16 * b + e] = y0.x; x[16 * b + e + 1] = y0.y; x[16 * b + e + 2] = y1.x; x[16 * b + e + 3] = y1.y;
-                    mx = max3(max3(mx, y0.x, y0.y), y1.x, y1.y);
                 }
+                triple_to_tmem(x_at + Z::X_STEP * b, x + 16 * b);
             }
             const float g_chunk = kco[3 * C];
-            *mine = mx;
-            if (meet()) { fail = true; break; }
-            if (Z::STAGE_V && leader) arrive(bar_vfree);
-            float inv_x;
-            pow2_scale(of_row(0), WIDE, sc, inv_x);
-#pragma unroll
-            for (int b = 0; b < TB; ++b) split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
             tc_wait_st();
             tc_fence_before();
             wait(bar_t(i), t_turn(i));
             if (meet()) { fail = true; break; }
+            if (Z::STAGE_V && leader) arrive(bar_vfree);
+            // T's or P's products, an operand in three parts on either side: what is below 2^-24 of the largest left out, small terms first
+            auto triangle = [&](uint32_t to, uint32_t from, const uint8_t* tile) {
+                const uint64_t at = tri_desc(uniform(smem_u32(tile)));
+                constexpr int PART[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+#pragma unroll
+                for (int t = 0; t < 6; ++t)
+#pragma unroll
+                    for (int ks = 0; ks < C / 16; ++ks)
+                        mma_ts(tmem_base + to + 16 * ks, tmem_base + from + Z::X_STEP * ks + 8 * PART[t][0], at + tri_step(ks) + ((PART[t][1] * TRI) >> 4),
+                               idesc_f16(C - 16 * ks) | BF16_OPERANDS, t != 0 || ks != 0);
+            };
             // ---- D = X T^T ----
             if (issuer) {
                 tc_fence_after();
-                const uint64_t td = umma_desc(uniform(smem_u32(t_ring + i % Z::T_STAGES * Z::T_BYTES)));
-#pragma unroll
-                for (int t = 2; t >= 0; --t)                      // small terms first: lo hi, hi lo, hi hi
-#pragma unroll
-                    for (int ks = 0; ks < C / 16; ++ks)
-                        mma_ts(tmem_base + Z::D_COL, tmem_base + Z::Z_COL + ks * 16 + (t == 2 ? 8 : 0), td + (((t == 1 ? TILE : 0) + ks * 32) >> 4), idesc_f16(C), t != 2 || ks);
+                triangle(Z::D_COL, 0, t_ring + i % Z::T_STAGES * TRI_BYTES);
                 mma_commit(bar_d);
+                mma_commit(bar_tfree(i));
             }
             wait_mma(bar_d, turn);
             tc_fence_after();
-            // ---- D's operands: times g_C / g (and what undoes the keys' scales) for the state, as it is for the outputs ----
-            float my = 0.f, me = 0.f;
+            // ---- D's operand for the state: times g_C / g (and what undoes the keys' scales) ----
+            float me = 0.f;
 #pragma unroll
             for (int b = 0; b < TB; ++b) {
                 uint32_t v[16];
@@ -684,19 +704,25 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     const float4 w = *reinterpret_cast<const float4*>(tco + TG * c + 16 * b + e);
                     const float2 d0 = pair(v[e], v[e + 1]), d1 = pair(v[e + 2], v[e + 3]), e0 = __fmul2_rn(d0, pair(w.x, w.y)), e1 = __fmul2_rn(d1, pair(w.z, w.w));
                     x[16 * b + e] = d0.x; x[16 * b + e + 1] = d0.y; x[16 * b + e + 2] = d1.x; x[16 * b + e + 3] = d1.y;
-                    my = max3(max3(my, d0.x, d0.y), d1.x, d1.y);
                     me = max3(max3(me, e0.x, e0.y), e1.x, e1.y);
                 }
             }
-            *mine = my;
             mine[G * ROWS] = me;
-            const float undo = inv_x * tco[2 * C];
             if (meet()) { fail = true; break; }
-            float inv_d, inv_e, sc_e;
-            pow2_scale(of_row(0), WIDE, sc, inv_d);
+            float inv_e, sc_e;
             pow2_scale(of_row(1), WIDE, sc_e, inv_e);
-            if (c == 0) inv_s[(2 + turn) * ROWS + r] = inv_d * undo;
-            const float back = (inv_e * undo) * scale_row;            // of D K, to the state rows' units
+            // the row's old part and what is added, in the units of the new one; where either would leave fp32's range in the old units (gates far beyond
+            // 1, values far above the state), smaller units
+            float keep = g_chunk;
+            if (fabsf(g_chunk) > 0x1p60f || (inv_e * 0x1p-64f) * (scale_row * 0x1p-64f) > 0x1p-68f) {
+                float down, up;
+                pow2_scale(fmaxf(fabsf(g_chunk), 1.f), 0, down, up);
+                const float scale_new = fmaxf(fminf(scale_row * down, sc_e), 0x1p-120f);
+                keep *= scale_new * inv_row;
+                inv_row = __uint_as_float((254u << 23) - __float_as_uint(scale_new));      // 1 / a power of two
+                scale_row = scale_new;
+            }
+            const float back = inv_e * scale_row;
 #pragma unroll
             for (int b = 0; b < TB; ++b) {
                 float y[16];
@@ -707,26 +733,14 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                     y[e] = e0.x; y[e + 1] = e0.y; y[e + 2] = e1.x; y[e + 3] = e1.y;
                 }
                 split_to_tmem(d_at + 16 * b, y, sc_e);
-                if constexpr (PARTS > 1) {
-                    split_to_tmem(z_at + 16 * b, x + 16 * b, sc);
-                } else {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 d = __fmul2_rn(pair(x[16 * b + 2 * e], x[16 * b + 2 * e + 1]), pair(sc, sc));
-                        w[e] = pack_f16x2(d.x, d.y);
-                    }
-                    tmem_st8(z_at + 16 * b, w);
-                }
             }
             tc_wait_st();
             tc_fence_before();
             if (meet()) { fail = true; break; }
-            // ---- D K over the S operand (read by now), and D P^T ----
+            // ---- D K over the X operand (read by now); D's operand for the outputs meanwhile, and D P^T ----
             if (issuer) {
                 tc_fence_after();
                 const uint64_t kd = umma_desc_mn(uniform(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES)), KQ_BLOCK);
-                const uint64_t pd = umma_desc(uniform(smem_u32(p_ring + i % Z::T_STAGES * Z::P_BYTES)));
                 bool first = true;
                 auto product = [&](int dp, int kp) {
 #pragma unroll
@@ -739,15 +753,18 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 product(1, 0);
                 product(0, 0);
                 mma_commit(bar_s);
+            }
 #pragma unroll
-                for (int t = PARTS > 1 ? 2 : 0; t >= 0; --t)
-#pragma unroll
-                    for (int ks = 0; ks < C / 16; ++ks)
-                        mma_ts(tmem_base + Z::O2_COL, tmem_base + Z::Z_COL + ks * 16 + (t == 2 ? 8 : 0), pd + (((t == 1 ? TILE : 0) + ks * 32) >> 4), idesc_f16(C),
-                               t != (PARTS > 1 ? 2 : 0) || ks);
+            for (int b = 0; b < TB; ++b) triple_to_tmem(do_at + Z::X_STEP * b, x + 16 * b);
+            tc_wait_st();
+            tc_fence_before();
+            meet();                                                   // (nobody has waited since the last one: nobody gives up here)
+            if (issuer) {
+                tc_fence_after();
+                triangle(Z::O2_COL, Z::DO_COL, p_ring + i % Z::P_STAGES * TRI_BYTES);
                 mma_commit(bar_o);
                 mma_commit(bar_kfree(i));
-                mma_commit(bar_tfree(i));
+                mma_commit(bar_pfree(i));
             }
             if (leader) arrive(bar_o);
             issued = i + 1;
@@ -761,7 +778,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    const float2 y2 = __ffma2_rn(pair(g_chunk, g_chunk), pair(S[16 * b + e], S[16 * b + e + 1]), __fmul2_rn(pair(v[e], v[e + 1]), pair(back, back)));
+                    const float2 y2 = __ffma2_rn(pair(keep, keep), pair(S[16 * b + e], S[16 * b + e + 1]), __fmul2_rn(pair(v[e], v[e + 1]), pair(back, back)));
                     S[16 * b + e] = y2.x;
                     S[16 * b + e + 1] = y2.y;
                     m = max3(m, y2.x, y2.y);
@@ -815,7 +832,6 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
         for (int i = -1; i < n && !fail; ++i) {                   // (-1: the first values only)
             const uint32_t turn = i & 1;
             const float* kco = kco_s + max(i, 0) % Z::K_STAGES * Z::KCO + C;
-            const float* tco = tco_s + max(i, 0) % Z::T_STAGES * Z::TCO + C;
             if (Z::STAGE_V && i + 1 < n) {
                 if (i >= 0) wait(bar_vfree, turn);
                 if (!fail) load_values(i + 1);
@@ -828,7 +844,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             wait(bar_o, turn);
             if (bar_or(OUT_BARRIER, 128, fail ? 1 : 0)) { fail = true; break; }
             tc_fence_after();
-            const float inv_row = inv_s[turn * ROWS + r], inv_d = inv_s[(2 + turn) * ROWS + r];
+            const float inv_row = inv_s[turn * ROWS + r];
             // read out first and stored behind that, so that the chain may go on (fp32: half of it, for want of registers)
             constexpr int PER = sizeof(T) == 2 ? 2 : 1, FIRST = PER == 2 ? 0 : 2;      // outputs per register; blocks of 16 stored at once
             T* dst = op + (long long)(i * C) * a.out_stride;
@@ -841,8 +857,8 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    const float2 gq = *reinterpret_cast<const float2*>(kco + 16 * b + e), ps = *reinterpret_cast<const float2*>(tco + 16 * b + e);
-                    const float2 y = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), pair(inv_row, inv_row)), gq, __fmul2_rn(__fmul2_rn(pair(w[e], w[e + 1]), pair(inv_d, inv_d)), ps));
+                    const float2 gq = *reinterpret_cast<const float2*>(kco + 16 * b + e);
+                    const float2 y = __ffma2_rn(__fmul2_rn(pair(v[e], v[e + 1]), pair(inv_row, inv_row)), gq, pair(w[e], w[e + 1]));
                     if constexpr (PER == 2) {
                         to[e / 2] = sm100::pack_bf16x2(y.x, y.y);
                     } else {
@@ -895,7 +911,6 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 store(16 * FIRST, C - 16 * FIRST, o);
             }
             arrive(bar_kfree(i));
-            arrive(bar_tfree(i));
         }
     }
     if (fail && a.status && atomicCAS(a.status, ONELA_OK, ONELA_E_TIMEOUT) == ONELA_OK) a.status[1] = sequence;
