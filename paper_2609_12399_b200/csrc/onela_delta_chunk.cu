@@ -13,7 +13,7 @@
 //
 // One CTA = (128 rows of the state, value head, sequence), all chunks of the sequence in order.  The state's rows lie in registers, a row in
 // two threads (a half each; dk = 64: four), one in each CHAIN warpgroup; all products have the rows as M = 128 lanes:
-//      S [K; Q]^T       one MMA set for Z and S Q^T (N = 128; the low half of S for Z alone where outputs are bf16)
+//      S [K; Q]^T       one MMA set for Z and S Q^T (N = 128)
 //      X T^T, D K, D P^T
 // PREPARING warpgroups take the chunks in turn: keys and queries to an operand tile (128 rows: 64 of K, 64 of Q), [K; Q] K^T in one MMA set,
 // A's and P's rows from it, T by blocks of 16 and joins, T and P as operand tiles.  An OUTPUT warpgroup brings the values into
@@ -26,8 +26,8 @@
 // has read them: a segment holds enough tokens for that, or its sequence is not cut.
 //
 // Precision.  S, X, D and the results are fp32.  Where a product runs over the state's columns (S [K; Q]^T, [K; Q] K^T) or into them (D K) an operand's row has one size
-// and its own power of two: operands are sums of two fp16 numbers (22 to 23 significant bits), keys and queries in bf16 one, exact; S in its product with bf16 queries
-// one as well (2^-11).  Along the tokens (T, P, X, D) sizes differ by what the gates have left, by far more than fp16's range: those operands are sums of three bf16 numbers (24 bits,
+// and its own power of two: operands are sums of two fp16 numbers (22 to 23 significant bits), keys and queries in bf16 one, exact.
+// (Outputs in bf16 see all of S and D too: a query along a key that is written over, o = S k + (v - S k), cancels what is large in both.)  Along the tokens (T, P, X, D) sizes differ by what the gates have left, by far more than fp16's range: those operands are sums of three bf16 numbers (24 bits,
 // fp32's range), with nothing to scale.  So what fades, or comes under a small key, keeps its places; only below 2^-110 they go.  (Two fp16 numbers with a scale per
 // row instead: outputs and states wrong in the third digit behind 64 gates of 0.8, in the first behind 64 of 0.6.)
 //
@@ -612,22 +612,17 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
                 tc_fence_after();
                 const uint64_t kd = umma_desc(uniform(smem_u32(smem + i % Z::K_STAGES * Z::KQ_BYTES)));
                 bool first = true;
-                auto product = [&](int sp, int kp, int cols) {
+                auto product = [&](int sp, int kp) {
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
                         const int kb = ks / KS;
-                        mma_ts(tmem_base + Z::Z_COL, tmem_base + ks * 16 + sp * 8, kd + ((((kp * KB + kb) * KQ_BLOCK) + (ks - kb * KS) * 32) >> 4), idesc_f16(cols), !first);
+                        mma_ts(tmem_base + Z::Z_COL, tmem_base + ks * 16 + sp * 8, kd + ((((kp * KB + kb) * KQ_BLOCK) + (ks - kb * KS) * 32) >> 4), idesc_f16(2 * C), !first);
                         first = false;
                     }
                 };
-                if constexpr (PARTS > 1) {
-                    product(1, 0, 2 * C);
-                    product(0, 1, 2 * C);
-                    product(0, 0, 2 * C);
-                } else {
-                    product(0, 0, 2 * C);
-                    product(1, 0, C);
-                }
+                product(1, 0);
+                if constexpr (PARTS > 1) product(0, 1);
+                product(0, 0);
                 mma_commit(bar_z);
             }
             float val[Z::STAGE_V ? 1 : TG];                       // fp32 values: from global memory, beside the product
