@@ -312,6 +312,9 @@ onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream)
  * tokens keeps its state (or, fresh, gets the zero state).  Found on the device, with *status_dev, if given, set to {ONELA_E_DEVICE_CHECK, sequence}
  * by one that finds it (the caller clears the words): a slot of num_states or more, or that an earlier sequence of the call has, and row
  * ranges that run backwards, begin before an earlier sequence's or leave [0, n_tokens]; such a sequence is treated as padded.
+ * The chunked kernel's waits are bounded.  One that runs out sets *status_dev to {ONELA_E_TIMEOUT, sequence} (the call itself has returned by then; without
+ * status_dev nothing tells): the outputs of that sequence are not to be used, and its state is per value head and 128 rows either the old or the new one, never one made
+ * of unfinished parts.  The other sequences are right, but of several that time out only the first is named.
  * States, outputs and inputs do not overlap.  In chunks, a token whose q, k, v or gates are not finite can make the outputs of up to 63 tokens before
  * it not finite too (what follows it is lost either way).
  * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it

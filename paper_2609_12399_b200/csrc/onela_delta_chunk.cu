@@ -40,7 +40,7 @@
 //   through shared memory (T and P in one tile each: 113 -> 157)
 //
 // Every wait is bounded: a thread that gives up raises the abort flag and keeps meeting its team's barriers, whose OR makes the team leave
-// together; ONELA_E_TIMEOUT goes to the caller's status word, if there is one.  Every MMA that was issued is waited for before tensor memory is freed.
+// together; ONELA_E_TIMEOUT goes to the caller's status word, if there is one, and no state is written that rests on what did not come about.  Every MMA that was issued is waited for before tensor memory is freed.
 #include <algorithm>
 #include <mutex>
 
@@ -146,6 +146,12 @@ __device__ __forceinline__ void triple_to_tmem(uint32_t taddr, const float* x) {
     tmem_st8(taddr + 16, w + 16);
 }
 
+#ifdef ONELA_TEST_HOOKS
+// Test-hooks build only (a second library that the product never loads): 1 + the part of a cut sequence (of sequence 0, value head 0) whose CTA of the maps'
+// launch gives up when all its work is done; 0: none.
+__device__ int g_hook_delta_map_fails;
+#endif
+
 enum { WHOLE, MAPS, OUTPUTS };
 
 // The part of a sequence that a CTA works on.
@@ -166,6 +172,14 @@ template <typename T>
 __device__ __forceinline__ float4* scratch(const DeltaArgs& a, long long row, int hv, int at) {
     const int per = a.dv * (int)sizeof(T) / 4, r = at / per;
     return reinterpret_cast<float4*>(reinterpret_cast<float*>(static_cast<T*>(a.out) + (row + r) * a.out_stride + (long long)hv * a.dv) + (at - r * per));
+}
+
+// A map may not come about (a wait that ran out); the launches behind it are queued by then.  So behind B and M a segment's rows hold whether both are there, [0] B, [1] M,
+// as MAPS found, and [2] whether the state before the segment can be, as FOLD concludes.  (The chunk that least_chunks adds has at least one token: room enough.)
+constexpr int32_t IS_THERE = 0x7e571;
+template <typename T>
+__device__ __forceinline__ int32_t* there(const DeltaArgs& a, long long row, int hv) {
+    return reinterpret_cast<int32_t*>(scratch<T>(a, row, hv, (a.dv + a.dk) * a.dk));
 }
 
 template <int D, typename T, int PHASE>
@@ -219,6 +233,7 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
     if (seg.count == 1 ? PHASE == MAPS || seg.p > 0 : identity && blockIdx.x > 0) return;
     seq.begin += seg.begin;
     seq.length = seg.length;
+    if (PHASE == OUTPUTS && seg.p > 0 && there<T>(a, seq.begin, hv)[2] != IS_THERE) return;     // (reported by MAPS; the state stays as it is)
     const int n = (seq.length + C - 1) / C;                                         // chunks
     if (tid == 0) {
         for (int s = 0; s < 3; ++s) {
@@ -784,7 +799,12 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             if (meet()) { fail = true; break; }
         }
         if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
+#ifdef ONELA_TEST_HOOKS
+        if (PHASE == MAPS && g_hook_delta_map_fails == 1 + part && sequence == 0 && hv == 0) fail = true;
+#endif
+        if (meet()) fail = true;                                  // (all of the state's rows or none)
         const bool last = PHASE == OUTPUTS && seg.p == seg.count - 1;
+        if (PHASE == MAPS && leader) there<T>(a, seq.begin + seq.length, hv)[identity ? 1 : 0] = fail ? 0 : IS_THERE;
         if (!fail && is_row && (PHASE != OUTPUTS || last)) {
             const long long next_row = seq.begin + seq.length;    // of the next segment: where a map goes
             int to_at = (identity ? a.dv * D + r * D : (row_base + r) * D) + c * H;
@@ -938,6 +958,12 @@ __global__ void __launch_bounds__(FOLD_THREADS) delta_fold_kernel(const DeltaArg
             sm100::cp_async16(smem_u32(M_s + (p & 1) * D * D + 4 * x), scratch<T>(a, at, hv, a.dv * D + 4 * x));
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    if (blockIdx.x == 0 && threadIdx.x < 32) {                                      // lane p: segment p
+        const int p = threadIdx.x;
+        int32_t* at = p > 0 && p < a.segments ? there<T>(a, row_of(p), hv) : nullptr;
+        const uint32_t missing = __ballot_sync(0xffffffffu, at && (at[0] != IS_THERE || (p > 1 && at[1] != IS_THERE)));
+        if (at) at[2] = missing << (31 - p) ? 0 : IS_THERE;
+    }
     fetch(1);
     for (int x = threadIdx.x; x < FOLD_ROWS * D / 4; x += FOLD_THREADS)             // the state before segment 1
         *reinterpret_cast<float4*>(S_s + 4 * x) = *scratch<T>(a, row_of(1), hv, row0 * D + 4 * x);
@@ -1011,6 +1037,10 @@ cudaError_t launch_d(const DeltaArgs& a, int32_t dtype, cudaStream_t stream) {
 }
 
 }  // namespace
+
+#ifdef ONELA_TEST_HOOKS
+extern "C" int onela_testhook_delta_map_fails(int part) { return (int)cudaMemcpyToSymbol(g_hook_delta_map_fails, &part, sizeof(int)); }
+#endif
 
 bool delta_chunk_supported(int32_t dk, int32_t) { return dk == 32 || dk == 64 || dk == 128; }
 
