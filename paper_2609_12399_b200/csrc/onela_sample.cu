@@ -60,7 +60,7 @@ struct Histograms {
 // What every CTA of a row knows.
 struct Row {
     float largest, zero_from;                    // what lies below zero_from has no mass
-    double scale, offset;                        // 256 log2(e) / T, and the same times - largest
+    double scale;                                // 256 log2(e) / T
     int places;                                  // F
     bool greedy;
 };
@@ -75,7 +75,8 @@ __device__ __forceinline__ int first_bin(const Row& r, float x) { return min(BIN
 // The weight in units of 2^-F: 2^F at the largest, 0 at -inf.  table[j] = 2^(j / 256).
 __device__ __forceinline__ u64 mass(const Row& r, const double* table, float x) {
     constexpr double MAGIC = 0x1.8p52, LN2 = 0x1.62e42fefa39efp-9;                      // (ln 2 / 256)
-    const double y = fma((double)x, r.scale, r.offset), t = y + MAGIC, f = (y - (t - MAGIC)) * LN2;
+    // (the difference first: scale times either side of it would leave the difference their rounding, 1e-9 of a mass where logits are 10^7 temperatures from 0)
+    const double d = (double)x - (double)r.largest, t = fma(d, r.scale, MAGIC), f = fma(d, r.scale, MAGIC - t) * LN2;
     const int n = __double2loint(t);
     const double w = table[n & (TABLE - 1)], v = fma(w, f * fma(f, fma(f, 1.0 / 6.0, 0.5), 1.0), w);
     const u64 m = __double2ull_rn(__hiloint2double(__double2hiint(v) + ((n >> 8) + r.places) * (1 << 20), __double2loint(v)));
@@ -222,9 +223,8 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
     const double inverse_t = 1.0 / (double)t;
     r.places = a.places;
     r.scale = inverse_t * (256.0 * 1.4426950408889634074);
-    r.offset = -(double)r.largest * r.scale;
-    // 2^(F + 1) of them make one unit.  (Where that lies below every float, or T is infinite: only -inf has none.)
-    r.zero_from = fmaxf((float)((double)r.largest - (a.places + 1) * 0.69314718055994530942 * (double)t), -FLT_MAX);
+    // 2^(F + 1) of them make one unit.  (Where that lies below every float, or T is infinite: only -inf has none.  Below +inf everything has none.)
+    r.zero_from = isinf(r.largest) ? r.largest : fmaxf((float)((double)r.largest - (a.places + 1) * 0.69314718055994530942 * (double)t), -FLT_MAX);
     const int k = a.top_k ? a.top_k[row] : 0;
     const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p_given = a.min_p ? a.min_p[row] : 0.f;
     const bool use_k = k >= 1 && k < a.vocab, use_p = top_p < 1.f;
