@@ -268,7 +268,8 @@ int32_t onela_uses_tensor_core_path(const onela_ctx* ctx);
  * and pointers are the caller's, every call is asynchronous on `stream` (a stream of the current device), allocates nothing
  * and can be captured in a CUDA graph.  Strides are in elements and at least the extent they step over; base pointers are
  * 16-byte aligned and, where a stride is given, so is every row (the stride times the element size is a multiple of 16) -
- * but for onela_sample_tokens, whose rows may start anywhere.
+ * but for onela_sample_tokens, whose rows may start at any element, and for arrays of one number per token, head, sequence or row (gates, positions, frequencies,
+ * slots, temperatures and the like), for which 4 bytes do.
  * Inputs and outputs do not overlap unless a call says so.  An empty call (no tokens, sequences or rows) does nothing. */
 
 #define ONELA_NORM_NONE 0

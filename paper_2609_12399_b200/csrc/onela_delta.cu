@@ -184,6 +184,7 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
     if (g->num_sequences > 65535 || g->num_v_heads > 65535 || g->n_tokens > 0x7fffff00ll) return ONELA_E_CAPACITY;
     if (!g->starts_dev && g->n_tokens != g->num_sequences) return ONELA_E_INVAL;
     if (!g->slots_dev && g->num_states < g->num_sequences) return ONELA_E_INVAL;
+    if (!aligned4(g->alpha_dev, g->beta_dev, g->starts_dev, g->slots_dev, g->fresh_dev, g->status_dev)) return ONELA_E_INVAL;
     if (g->num_sequences == 0) return ONELA_OK;
     const long long es = g->dtype == ONELA_DTYPE_BF16 ? 2 : 4, big = 1ll << 40;
     auto rows = [](const void* p, long long stride, long long extent, long long size, long long n) {

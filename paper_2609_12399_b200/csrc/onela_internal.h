@@ -238,6 +238,9 @@ cudaError_t launch_decode_wy(const DecodeArgs& a, int32_t out_dtype, cudaStream_
 
 // ---- arguments of the operators without a context ----
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// Whether all of them (floats and 32-bit integers that kernels read or write one by one; null counts) lie on their own boundaries.
+template <typename... P>
+bool aligned4(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0; }
 // Rows [base + i stride, + extent) in bytes, i < n
 struct Rows {
     const char* base;

@@ -252,7 +252,7 @@ extern "C" onela_status onela_norm_rotate(const onela_norm_rotate_args* g, void*
     if (g->n_tokens == 0 || (g->num_q_heads == 0 && g->num_k_heads == 0)) return ONELA_OK;
     if (g->n_tokens > 0x7fffffffll || g->num_q_heads > MAX_HEADS || g->num_k_heads > MAX_HEADS) return ONELA_E_CAPACITY;      // CTAs of one launch, 32-bit offsets within a token
     if (g->rotary_dim > 0 && (!g->positions_dev || !g->inv_freq_dev)) return ONELA_E_INVAL;
-    if (!aligned16(g->q_weight_dev) || !aligned16(g->k_weight_dev)) return ONELA_E_INVAL;
+    if (!aligned16(g->q_weight_dev) || !aligned16(g->k_weight_dev) || !aligned4(g->positions_dev, g->inv_freq_dev)) return ONELA_E_INVAL;
     const Rows set[4] = {{static_cast<const char*>(g->q_dev), g->q_stride * es, (long long)g->num_q_heads * g->head_dim * es, g->n_tokens},
                          {static_cast<const char*>(g->k_dev), g->k_stride * es, (long long)g->num_k_heads * g->head_dim * es, g->n_tokens},
                          {static_cast<const char*>(g->q_out_dev), g->q_out_stride * es, (long long)g->num_q_heads * g->head_dim * es, g->n_tokens},

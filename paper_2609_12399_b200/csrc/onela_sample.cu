@@ -655,6 +655,7 @@ extern "C" onela_status onela_sample_tokens(const onela_sample_args* g, void* st
     if (g->rows == 0) return ONELA_OK;
     if (!g->logits_dev || !g->uniforms_dev || !g->tokens_out_dev || (g->logits_stride != 0 && g->logits_stride < g->vocab)) return ONELA_E_INVAL;
     if (reinterpret_cast<uintptr_t>(g->logits_dev) % (g->dtype == ONELA_DTYPE_BF16 ? 2 : 4) != 0) return ONELA_E_INVAL;
+    if (!aligned4(g->uniforms_dev, g->temperature_dev, g->top_p_dev, g->min_p_dev, g->top_k_dev, g->tokens_out_dev, g->logprobs_out_dev)) return ONELA_E_INVAL;
     int log_vocab = 0;
     while ((1ll << log_vocab) < g->vocab) ++log_vocab;
     const SampleArgs a{g->logits_dev, g->uniforms_dev, g->temperature_dev, g->top_p_dev, g->min_p_dev, g->top_k_dev, g->tokens_out_dev, g->logprobs_out_dev,
