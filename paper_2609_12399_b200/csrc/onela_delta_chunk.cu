@@ -798,14 +798,14 @@ __global__ void __launch_bounds__(Shape<D, T>::THREADS, 1) delta_chunk_kernel(co
             tc_fence_before();
             if (meet()) { fail = true; break; }
         }
-        if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
 #ifdef ONELA_TEST_HOOKS
         if (PHASE == MAPS && g_hook_delta_map_fails == 1 + part && sequence == 0 && hv == 0) fail = true;
 #endif
-        if (meet()) fail = true;                                  // (all of the state's rows or none)
+        const bool come = !fail;                                  // (the same in all of the chain's threads, who have met since they last waited for what S needs)
+        if (issued > 0) wait_mma(bar_o, (issued - 1) & 1);        // (the outputs' products too are over when tensor memory is freed)
         const bool last = PHASE == OUTPUTS && seg.p == seg.count - 1;
-        if (PHASE == MAPS && leader) there<T>(a, seq.begin + seq.length, hv)[identity ? 1 : 0] = fail ? 0 : IS_THERE;
-        if (!fail && is_row && (PHASE != OUTPUTS || last)) {
+        if (PHASE == MAPS && leader) there<T>(a, seq.begin + seq.length, hv)[identity ? 1 : 0] = come ? IS_THERE : 0;
+        if (come && is_row && (PHASE != OUTPUTS || last)) {
             const long long next_row = seq.begin + seq.length;    // of the next segment: where a map goes
             int to_at = (identity ? a.dv * D + r * D : (row_base + r) * D) + c * H;
             asm volatile("" : "+r"(to_at));                       // (not to be worked out ahead of the loop, which needs the registers)
