@@ -22,10 +22,12 @@ namespace onela {
 namespace {
 
 constexpr int WARPS = 4;
-// Tokens of the longest sequence from which the chunked kernel is the faster one.  Measured, us token by token / in chunks: 128 x 128 bf16, 16 heads, one
-// sequence of 24 11.3 / 18.3, 32 14.4 / 18.4, 48 20.6 / 18.4; four of 24 17.3 / 18.6, 32 22.1 / 18.6; 37 of 24 72 / 74, 32 93 / 75; 32 heads, four of 16
-// 20.3 / 19.1; 64 x 64 fp32, 16 heads, one of 32 10.6 / 13.6, 48 15.0 / 13.7, 37 of 32 39.6 / 55, 64 74 / 56.
-constexpr int CHUNKED_FROM = 32;
+// Tokens of the longest sequence from which the chunked kernel is the faster one.  Measured, us token by token / in chunks, 16 heads, one sequence, four, 37:
+// 128 x 128 bf16, 24 tokens 11.3 / 18.7, 17.3 / 19.1, 72 / 76; 32: 14.5 / 18.8, 22.2 / 19.2, 93 / 77; 48: 20.5 / 19.1, 31.6 / 19.5, 135 / 78 (32 heads, four of 16:
+// 20.2 / 19.5); 128 x 128 fp32, 32 tokens 11.0 / 19.1, 19.0 / 19.4, 88 / 79; 64 x 64 bf16, 24 tokens 10.6 / 12.7, 11.1 / 13.0, 42 / 53; 32: 13.6 / 12.8, 14.1 / 13.1, 54 / 53.
+// Narrow heads in fp32 take fewer instructions token by token and more in chunks: 64 x 64, 40 tokens 12.9 / 13.7, 13.5 / 14.0, 48 / 56; 48: 15.2 / 13.7, 15.7 / 14.0, 57 / 56;
+// 32 x 32, 40 tokens 12.4 / 11.4, 12.8 / 11.8, 45 / 47.
+inline long long chunked_from(int32_t dtype, int32_t dk) { return dtype == ONELA_DTYPE_F32 && dk <= 64 ? 44 : 32; }
 
 template <typename T>
 __device__ __forceinline__ void load4(const T* p, float* x);
@@ -204,7 +206,7 @@ extern "C" onela_status onela_delta_rule(const onela_delta_rule_args* g, void* s
                       g->num_sequences, g->num_states, g->num_heads, g->num_v_heads, g->dv, g->dk, 1};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const long long longest = !g->starts_dev ? 1 : g->max_tokens > 0 ? g->max_tokens : g->n_tokens;
-    const cudaError_t e = longest >= CHUNKED_FROM && delta_chunk_supported(g->dk, g->dv) ? launch_delta_chunk(a, g->dtype, longest, s)
+    const cudaError_t e = longest >= chunked_from(g->dtype, g->dk) && delta_chunk_supported(g->dk, g->dv) ? launch_delta_chunk(a, g->dtype, longest, s)
                           : g->dtype == ONELA_DTYPE_BF16 ? launch_step_t<__nv_bfloat16>(a, s) : launch_step_t<float>(a, s);
     return e == cudaSuccess ? ONELA_OK : ONELA_E_CUDA;
 }
