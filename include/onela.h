@@ -283,7 +283,7 @@ int32_t onela_uses_tensor_core_path(const onela_ctx* ctx);
  * position * inv_freq[i]: (a, b) -> (a cos - b sin, b cos + a sin).  Angles are formed in 64 bits and any int32 position is
  * fine, negative ones included.  Queries are multiplied by q_scale at the end.  Norms and products in fp32, one rounding.
  * q_out may be q and k_out may be k with the same stride (in place); otherwise outputs overlap nothing.  More than 2^31 - 1 tokens or 2^20
- * heads of queries or of keys: ONELA_E_CAPACITY. */
+ * heads of queries or of keys: ONELA_E_CAPACITY.  Sums of squares beyond fp32's range give zeros. */
 typedef struct onela_norm_rotate_args {
     const void *q_dev, *k_dev;        /* [n_tokens][num_q_heads][head_dim], [n_tokens][num_k_heads][head_dim] in dtype */
     void *q_out_dev, *k_out_dev;      /* the same shapes and dtype */
@@ -316,10 +316,14 @@ onela_status onela_norm_rotate(const onela_norm_rotate_args* args, void* stream)
  * The chunked kernel's waits are bounded.  One that runs out sets *status_dev to {ONELA_E_TIMEOUT, sequence} (the call itself has returned by then; without
  * status_dev nothing tells): the outputs of that sequence are not to be used, and its state is per value head and 128 rows either the old or the new one, never one made
  * of unfinished parts.  The other sequences are right, but of several that time out only the first is named.
- * States, outputs and inputs do not overlap.  In chunks, a token whose q, k, v or gates are not finite can make the outputs of up to 63 tokens before
+ * States, outputs and inputs do not overlap.  In chunks, a token whose q, k, v or gates are not finite can make the outputs of up to 15 tokens before
  * it not finite too (what follows it is lost either way).
- * max_tokens: what the caller expects the longest sequence to have (0: n_tokens); results hold whatever it says, but it
- * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores.
+ * max_tokens: what the caller expects the longest sequence to have (0: n_tokens; so batches of single tokens given by `starts` should say 1).  It
+ * chooses between a kernel that steps token by token and one that works in chunks of 64 tokens on the tensor cores, where every sequence takes a whole
+ * number of chunks; with the number of sequences and heads it decides too whether long sequences are cut.  Results hold whatever it says, to fp32's precision and not bit
+ * for bit: an output, before its rounding to dtype, is off by some 2^-22 of |S| |q| and of the terms that the last 64 tokens add to it, as far as they have decayed, token by token by
+ * 2^-24 per step of |S| |q|; a state likewise.  In chunks magnitudes below 2^-110 may be lost, and what a running product of up to 64 gates carries beyond 2^120 may
+ * become infinite.
  * (dk, dv): multiples of 32 with dk in {32, 64, 128, 256}, dv up to 512, else ONELA_E_UNSUPPORTED.
  * At most 65 535 sequences, 65 535 value heads and 2^31 - 256 tokens, else ONELA_E_CAPACITY. */
 typedef struct onela_delta_rule_args {

@@ -25,19 +25,20 @@
 // segment from its state.  The state before a segment, its predecessor's B before that, and M lie meanwhile in the segment's own rows of the caller's `out`, which OUTPUTS overwrites when it
 // has read them: a segment holds enough tokens for that, or its sequence is not cut.
 //
-// Precision.  S, X, D and the results are fp32.  Where a product runs over the state's columns (S [K; Q]^T, [K; Q] K^T) or into them (D K) an operand's row has one size
-// and its own power of two: operands are sums of two fp16 numbers (22 to 23 significant bits), keys and queries in bf16 one, exact.
-// (Outputs in bf16 see all of S and D too: a query along a key that is written over, o = S k + (v - S k), cancels what is large in both.)  Along the tokens (T, P, X, D) sizes differ by what the gates have left, by far more than fp16's range: those operands are sums of three bf16 numbers (24 bits,
-// fp32's range), with nothing to scale.  So what fades, or comes under a small key, keeps its places; only below 2^-110 they go.  (Two fp16 numbers with a scale per
-// row instead: outputs and states wrong in the third digit behind 64 gates of 0.8, in the first behind 64 of 0.6.)
+// Precision.  S, X, D and the results are fp32.  Where a product runs over the state's columns (S [K; Q]^T, [K; Q] K^T) or into them (D K) an operand's row has
+// one size and its own power of two: operands are sums of two fp16 numbers (22 to 23 significant bits), keys and queries in bf16 one, exact.  (Outputs in bf16
+// see all of S and D too: a query along a key that is written over, o = S k + (v - S k), cancels what is large in both.)  Along the tokens (T, P, X, D) sizes differ
+// by what the gates have left, by far more than fp16's range: those operands are sums of three bf16 numbers (24 bits, fp32's range), with nothing to scale.  So
+// what fades, or comes under a small key, keeps its places; only below 2^-110 they go.  (Two fp16 numbers with a scale per row instead: outputs and states wrong
+// in the third digit behind 64 gates of 0.8, in the first behind 64 of 0.6.)
 //
-// What bounds it: a chunk takes a CTA 11 000 cycles (5.9 us), of which the chain of its products and their operands is the critical path, and 24 000 warp
-// instructions (issue slots 56 % used; the preparation 8 500 of them, the chain twelve, the outputs three thousand).  With both SMs of a pair at work it was 8.4 us,
-// and each kilobyte less of code brought that down (126 KB 182 us, 98 KB 153 us for 9 x 1408 tokens x 16 heads): they share an instruction
-// cache.  4096 tokens x 16 heads of 128 x 128 bf16: 3069 us token by token, 360 in chunks, 220 in six segments.
-//   taken back or worse: MMA descriptors not known to be uniform (16 MMAs 5450 cycles instead of 1000), outputs stored before the accumulators are
-//   given back (period + 60 %), P's rows by their true largest element (two rounds), four chain warpgroups at dk = 128 (381 -> 401), values of fp32
-//   through shared memory (T and P in one tile each: 113 -> 157)
+// What bounds it: a chunk takes a CTA 6.5 us (128 x 128 bf16, 16 CTAs; 7.1 with 64, 7.7 with 144, both SMs of a pair at work, which share an instruction cache; fp32 9.7, 64 x 64
+// bf16 5.6, fp32 6.1).  The chain of its products and their operands is the critical path; 25 000 warp instructions, issue slots 52 % used, the tensor pipe 23 %.  4096 tokens x 16
+// heads of 128 x 128 bf16: 3069 us token by token, 393 in chunks, 230 in six segments.
+//   taken back or worse: D's operand for the outputs written before D K is issued (128 x 128 bf16 6.5 us -> 6.9), the six products of a triangle in a loop (+ 10 %:
+//   descriptors), a barrier behind the chain's loop (the compiler lays the loop out differently: 6.5 -> 9.9); with two fp16 parts along the tokens: MMA descriptors not known to be uniform
+//   (16 MMAs 5450 cycles instead of 1000), outputs stored before the accumulators are given back (period + 60 %), four chain warpgroups at dk = 128 (4096 tokens 381 -> 401),
+//   values of fp32 through shared memory (T and P in one tile each: 113 -> 157)
 //
 // Every wait is bounded: a thread that gives up raises the abort flag and keeps meeting its team's barriers, whose OR makes the team leave
 // together; ONELA_E_TIMEOUT goes to the caller's status word, if there is one, and no state is written that rests on what did not come about.  Every MMA that was issued is waited for before tensor memory is freed.

@@ -6,7 +6,7 @@
 // A row is one (token, head); 4 to 32 lanes share it, one or two pieces of 8 elements (16 bytes of bf16, 32 of fp32) each, and a thread has four
 // pieces in flight.
 // A CTA takes a few whole tokens, queries' and keys' heads alike: as many as leave the fewest passes of rows one after
-// another (18 heads of 256 in passes of 32 rows: 16 tokens are 9 full passes, one token would leave 14 of 32 rows idle).  The angles belong to the token:
+// another (18 heads of 256 in passes of 32 rows: 7 tokens fill 126 of the rows of four passes, one token would leave 14 of 32 idle).  The angles belong to the token:
 // cosine and sine are formed once per CTA, in shared memory.  position * inv_freq is exact in 64 bits (31 + 24 bits; two more than fit are
 // rounded), reduced there to a fraction of a turn, and only the fraction goes through the fp32 functions, so far positions lose nothing.
 // Measured: 16 384 tokens x 64 heads of 128 80.5 us (6.7 TB/s, the copy's rate; one piece per lane 92, 64-bit row numbers and a division per row

@@ -36,7 +36,7 @@ namespace cg = cooperative_groups;
 using u64 = unsigned long long;
 
 constexpr int MAX_THREADS = 1024, TABLE = 256, BINS = 896, FINE = 512, MAX_SLICE = 50048, MAX_CLUSTER = 8, MAX_VOCAB = 360000;
-constexpr float BINS_PER_UNIT = 32.f;            // first histogram: bins of 1 / 32 up to 32 below the largest, the rest in the last one
+constexpr float BINS_PER_UNIT = 32.f;            // first histogram: bins of 1 / 32 up to 28 below the largest, the rest in the last one
 
 struct SampleArgs {
     const void* logits;
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(MAX_THREADS) sample_kernel(const SampleArgs a)
 #pragma unroll
         for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4*>(x_s + u * VE + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
     };
-    // whole vectors, eight on their way at a time; the row's first and last one by elements
+    // whole vectors, four on their way at a time; the row's first and last one by elements
     const int whole0 = unit0 == 0 && skip > 0 ? 1 : 0, whole1 = n / VE - (unit0 + n / VE == units && end % VE != 0 ? 1 : 0);
     constexpr int BATCH = 4;
     for (int u0 = whole0 + tid; u0 < whole1; u0 += threads * BATCH) {

@@ -170,3 +170,26 @@ def test_long_sequences_whose_maps_fade(dtype):
         x["alpha"][:] = alpha
         x["v"][:2300] = 0
         _check(**x, dtype=dtype, max_tokens=0)
+
+
+@pytest.mark.parametrize("max_tokens", [1, 0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("what", ["q", "k", "v", "alpha", "beta"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_token_that_is_not_finite_reaches_back_15_tokens_at_most(value, what, dtype, max_tokens):
+    """Token 110 of 150: what lies before token 96 is what it is without it, bit for bit."""
+    x = _inputs(150, seed=7)
+    outs = []
+    for bad in (False, True):
+        y = {n: t.clone() for n, t in x.items()}
+        if bad:
+            y[what][110] = value
+        dev = {n: t.to(device="cuda", dtype=DT[dtype] if n in "qkv" else torch.float32) for n, t in y.items()}
+        states, out = dev["S"][None].clone(), torch.zeros_like(dev["v"])
+        P.onela_delta_rule(dev["q"], dev["k"], dev["v"], dev["alpha"], dev["beta"], states, out, starts=torch.tensor([0, 150], dtype=torch.int32, device="cuda"), max_tokens=max_tokens)
+        torch.cuda.synchronize()
+        outs.append(out)
+    assert torch.isfinite(outs[0]).all()
+    assert torch.equal(outs[0][:96], outs[1][:96])
+    if max_tokens == 1:
+        assert torch.equal(outs[0][:110], outs[1][:110])
